@@ -113,6 +113,21 @@ size_t sd_kv_bytes(const sd_config* cfg, int32_t batch, int32_t cap);
 int sd_kv_create(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes,
                  sd_kv** out);
 int sd_kv_destroy(sd_kv* kv);
+/* A cache that holds its rows in 8 bits: half the bytes to keep and to read at long contexts. bfloat16 models only (SD_ERR_SHAPE
+ * otherwise; sd_kv8_bytes returns 0). The handle is an sd_kv like any other: every call that takes one takes this one, steps,
+ * prompts and commits included; arguments as sd_kv_create's. What differs:
+ *   - A block of 32 rows (0..31, 32..63, ..) of one head, keys and values apart, has one exponent e: the least whole number with
+ *     max|x| <= 448 * 2^e over the block's rows (0 for a block of zeros; -100 <= e <= 120). It holds x / 2^e rounded to the nearest
+ *     e4m3 number (4 exponent bits, 3 mantissa bits, largest 448; ties to even), and a row that is read is that number * 2^e, which
+ *     bfloat16 holds exactly. Infinities and NaN become NaN and have no say in e.
+ *   - A block that gets further rows gets a new exponent; the values it holds stay as they are, save those below 2^-15 of its
+ *     largest, which lose low bits. Rows past the committed length have no say in the exponent when a step or a prompt commits
+ *     rows, and saturate at the block's largest number; sd_kv_write_rows counts all rows of a block that it does not overwrite.
+ *   - Steps attend the rounded rows (queries and probabilities in one bfloat16 term), their own tree's rows in bfloat16. Prompts
+ *     run in passes of up to 256 rows, each committed before the next. sd_set_fused has no effect.                              */
+size_t sd_kv8_bytes(const sd_config* cfg, int32_t batch, int32_t cap);
+int sd_kv8_create(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes,
+                  sd_kv** out);
 /* Committed length per sequence -> host out_len[batch]. Synchronises `stream`.              */
 int sd_kv_len(sd_kv* kv, int32_t* out_len, void* stream);
 /* Set the committed length per sequence from host len[batch] (roll back after a step, or
@@ -128,6 +143,30 @@ int sd_kv_write_rows(sd_kv* kv, int32_t layer, int32_t seq, int32_t row0, int32_
                      const void* k_rows, const void* v_rows, void* stream);
 int sd_kv_read_rows(sd_kv* kv, int32_t layer, int32_t seq, int32_t row0, int32_t nrows,
                     void* k_rows, void* v_rows, void* stream);
+/* The same rows of every layer in one call (a sequence saved, moved to another process or put back): arrays
+ * [n_layers][nrows][n_heads][head_dim].                                                     */
+int sd_kv_write_layers(sd_kv* kv, int32_t seq, int32_t row0, int32_t nrows, const void* k_rows,
+                       const void* v_rows, void* stream);
+int sd_kv_read_layers(sd_kv* kv, int32_t seq, int32_t row0, int32_t nrows, void* k_rows, void* v_rows,
+                      void* stream);
+/* Branch a sequence: the committed rows of sequence src_seq of `src`, its length and its carried draft state replace those of
+ * the n_dst sequences dst_seqs (host, read during the call) of `dst`, each of which then goes on by itself (n samples of one
+ * prompt; a prompt run in a cache of its own that joins a running batch). `dst` may be `src` (then src_seq is not among
+ * dst_seqs). Both caches belong to one model (SD_ERR_STATE) and store rows alike (SD_ERR_SHAPE); no sequence is named twice.
+ * SD_ERR_KV_FULL if the rows might not fit (judged from the length that the host knows). SD_ERR_STATE for a stream under capture.
+ * The tree rows of the last pass stay those of the sequences that the pass held.            */
+int sd_kv_fork(sd_kv* src, int32_t src_seq, sd_kv* dst, const int32_t* dst_seqs, int32_t n_dst, void* stream);
+/* Drop rows from a sequence and close the gaps (a full cache goes on without a part of its context): rows first[i] ..
+ * first[i] + count[i] - 1 for n_ranges ranges (host arrays, read during the call; ascending, apart from one another, inside the
+ * cache's capacity; 1 <= n_ranges <= SD_MAX_DROP_RANGES). The rows behind move up, in place, and their keys are rotated on to their
+ * new positions (frequencies of the model, in float64, rounded once to the storage format), so that the sequence is what it would be
+ * with those rows at those positions. Rows at or past the committed length count as none. The carried draft state stays; tree rows
+ * of an earlier pass (sd_kv_commit_rows) were rotated for the old length. The sequence's other blocks are not touched; 8-bit blocks
+ * from the first dropped row on are rounded anew, with the exponent of the rows they now hold.
+ * SD_ERR_STATE for a stream under capture.                                                  */
+#define SD_MAX_DROP_RANGES 16
+int sd_kv_drop_rows(sd_kv* kv, int32_t seq, const int32_t* first, const int32_t* count, int32_t n_ranges,
+                    void* stream);
 /* Overwrite the carried draft state of every sequence: the base model's token for the next
  * position (dev root_tok[batch]) and the heads' candidates (dev cand[batch][n_medusa][topk]).
  * Used with synthetic caches, and to resynchronise a lock-step comparison. Both arrays are
@@ -211,6 +250,17 @@ int sd_verify_tree(const sd_tree* tree, int32_t batch, int32_t n_medusa, int32_t
                    int32_t* n_accept, int32_t* n_accept_raw, int32_t* tokens, int32_t* src_slots,
                    void* stream);
 
+/* Tree attention alone, over a cache in 8 bits: for every sequence b and node t,
+ *   out[b][t] = sum_j softmax_j(q[b][t] . key_j / sqrt(head_dim)) value_j
+ * per head, j over the committed rows of layer `layer` and over t's ancestors in the tree and t itself. q, k, v: dev bfloat16 rows
+ * [batch * T] of n_heads * head_dim contiguous elements, `ld` elements apart (three parts of one packed projection, say), already
+ * rotated (sd_rope_rows; node t stands at the committed length + its depth); out likewise, ld_out apart, written in full. All
+ * 16-byte aligned, ld and ld_out multiples of 8 (SD_ERR_SHAPE); out overlaps none of the others. Float32 scores, sums and
+ * accumulation, probabilities rounded to bfloat16 for the second product. Touches no state; batch * round_up(T, 32) rows must
+ * fit the model's max_rows. The launch is cut by the lengths that the host knows.             */
+int sd_tree_attention(sd_model* m, sd_kv* kv, const sd_tree* tree, int32_t layer, const void* q, const void* k,
+                      const void* v, int32_t ld, void* out, int32_t ld_out, void* stream);
+
 /* Commit of key/value rows alone (the last stage of a step, Section III-B: the accepted tokens become part of the
  * sequence): for every sequence b of `kv`, rows src_slots[b][0 .. n_rows[b]) of the tree rows that the LAST step or
  * prefill chunk of this model over this cache's batch computed are appended to the cache, in that order, and the
@@ -250,6 +300,39 @@ int sd_verify_tree_typical_static(const sd_tree* tree, int32_t batch, int32_t n_
  * out[i] = -1 for a row index outside [0, n_rows).                                           */
 int sd_sample_tokens(const float* logits, int32_t n_rows, int32_t ld, int32_t vocab, const int32_t* rows,
                      const float* u, int32_t n, float temperature, int32_t* out, void* stream);
+
+/* ---- rotary positions -------------------------------------------------------------------------
+ * Pair i of a head's first rotary_dim dims, (a, b), becomes magnitude * (a cos w - b sin w, a sin w + b cos w), w = position * f_i,
+ * f_i = theta^(-2 i / rotary_dim). Pairs are (i, i + rotary_dim / 2) (SD_ROPE_HALF, the model's own) or (2 i, 2 i + 1)
+ * (SD_ROPE_INTERLEAVED). For contexts longer than the trained one the frequencies are scaled: SD_ROPE_LINEAR f_i / factor;
+ * SD_ROPE_BY_PARTS f_i * (g + (1 - g) / factor), g = (trained_len f_i / 2 pi - low) / (high - low) clamped to 0..1: pairs that
+ * turn more than `high` times within the trained length stay, those that turn less than `low` times are divided. */
+#define SD_ROPE_HALF        0
+#define SD_ROPE_INTERLEAVED 1
+#define SD_ROPE_PLAIN       0
+#define SD_ROPE_LINEAR      1
+#define SD_ROPE_BY_PARTS    2
+typedef struct sd_rope {
+    float theta;               /* > 0                                                         */
+    int32_t rotary_dim;        /* even, 2..256, at most head_dim                              */
+    int32_t layout;            /* SD_ROPE_HALF or SD_ROPE_INTERLEAVED                         */
+    int32_t scaling;           /* SD_ROPE_PLAIN, SD_ROPE_LINEAR or SD_ROPE_BY_PARTS           */
+    float factor;              /* > 0; not read by SD_ROPE_PLAIN                              */
+    float low, high;           /* low < high; SD_ROPE_BY_PARTS only                           */
+    int32_t trained_len;       /* >= 1; SD_ROPE_BY_PARTS only                                 */
+    float magnitude;           /* > 0: factor of every cosine and sine (1: none)              */
+} sd_rope;
+/* Rows rotated to their positions: x, y dev [n_rows] of n_heads * head_dim contiguous elements (n_heads <= 1024, head_dim <= 1024)
+ * of `dtype` (SD_DTYPE_BF16 or SD_DTYPE_F32), ld_x / ld_y elements apart; y may be x (with ld_y = ld_x), else they do not overlap.
+ * pos: dev int32 [n_rows], any value. inverse: rotates by -w, which is the gradient of the rotation with respect to x. Dims past
+ * rotary_dim are copied. Angles are taken in float64, products in float32. n_rows = 0 does nothing. Rows that are 16-byte aligned,
+ * with rotary_dim a multiple of 16 and head_dim of 8, move fastest. The queries and keys of a packed projection are one call. */
+int sd_rope_rows(const sd_rope* rope, int32_t dtype, const void* x, int64_t ld_x, void* y, int64_t ld_y,
+                 const int32_t* pos, int32_t n_rows, int32_t n_heads, int32_t head_dim, int32_t inverse, void* stream);
+/* The model's own steps and prompts with other frequencies, from the next one on `stream` on (rotary_dim = head_dim, SD_ROPE_HALF;
+ * SD_ERR_SHAPE otherwise; SD_ERR_STATE for a stream under capture). Captured step graphs follow. Keys that are in a cache already
+ * were rotated with the old ones: call it before the first prompt.                           */
+int sd_set_rope(sd_model* m, const sd_rope* rope, void* stream);
 
 /* ---- training-side data preparation ----------------------------------------------------------
  * Syntax-enriched labels (Section III-C, Fig. 3). l0: dev int32 [batch][seq], the base model's

@@ -15,6 +15,8 @@ EXPORTED_SYMBOLS = [
     "sd_kv_set_len", "sd_kv_write_rows", "sd_kv_read_rows", "sd_kv_set_draft", "sd_kv_get_draft",
     "sd_tree_create", "sd_tree_destroy", "sd_prefill", "sd_spec_step", "sd_greedy_step", "sd_verify_tree",
     "sd_kv_commit_rows", "sd_spec_step_typical", "sd_verify_tree_typical", "sd_verify_tree_typical_static", "sd_sample_tokens", "sd_build_labels",
+    "sd_kv8_bytes", "sd_kv8_create", "sd_kv_write_layers", "sd_kv_read_layers", "sd_kv_fork", "sd_kv_drop_rows", "sd_tree_attention",
+    "sd_rope_rows", "sd_set_rope",
     "sd_set_graph_mode", "sd_set_draft_schedule", "sd_set_greedy_drafts", "sd_set_fused", "sd_set_sync_timeout", "sd_set_layer_timeline", "sd_profile_begin", "sd_profile_end", "sd_last_error", "sd_version",
 ]
 
@@ -49,6 +51,11 @@ class _StepIO(C.Structure):
 class _Typical(C.Structure):
     _fields_ = [("temperature", C.c_float), ("epsilon", C.c_float), ("delta", C.c_float), ("u", C.c_void_p),
                 ("row_stats", C.c_void_p)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("theta", C.c_float), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("factor", C.c_float),
+                ("low", C.c_float), ("high", C.c_float), ("trained_len", C.c_int32), ("magnitude", C.c_float)]
 
 
 def lib_path() -> str:
@@ -96,6 +103,19 @@ def lib() -> C.CDLL:
         L.sd_sample_tokens.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
                                        C.c_float, C.c_void_p, C.c_void_p]
         L.sd_build_labels.argtypes = [C.c_void_p] + [C.c_int32] * 7 + [C.c_void_p, C.c_void_p]
+        L.sd_kv8_bytes.restype = C.c_size_t
+        L.sd_kv8_bytes.argtypes = L.sd_kv_bytes.argtypes
+        L.sd_kv8_create.argtypes = L.sd_kv_create.argtypes
+        layers = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.sd_kv_write_layers.argtypes = layers
+        L.sd_kv_read_layers.argtypes = layers
+        L.sd_kv_fork.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, i32p, C.c_int32, C.c_void_p]
+        L.sd_kv_drop_rows.argtypes = [C.c_void_p, C.c_int32, i32p, i32p, C.c_int32, C.c_void_p]
+        L.sd_tree_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                        C.c_void_p, C.c_int32, C.c_void_p]
+        L.sd_rope_rows.argtypes = [C.POINTER(_Rope), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
+                                   C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
+        L.sd_set_rope.argtypes = [C.c_void_p, C.POINTER(_Rope), C.c_void_p]
         L.sd_profile_begin.argtypes = [C.c_void_p, C.c_int32]
         L.sd_set_graph_mode.argtypes = [C.c_void_p, C.c_int32]
         L.sd_set_draft_schedule.argtypes = [C.c_void_p, C.c_int32]
@@ -131,6 +151,26 @@ def _config(shape, trunc_fallback: str) -> _Config:
     return _Config(shape.n_layers, shape.d_model, shape.n_heads, shape.head_dim, shape.d_ffn, shape.vocab,
                    shape.n_medusa, shape.topk, 1 if shape.dtype == "bf16" else 0,
                    {"keep_all": 0, "keep_one": 1}[trunc_fallback], shape.rope_theta, shape.rms_eps)
+
+
+@dataclass(frozen=True)
+class Rope:
+    """sd_rope: how positions turn the pairs of a head's first `rotary_dim` dims. layout "half" | "interleaved", scaling "none" |
+    "linear" | "by_parts" (`factor`; by parts also `low`, `high`, `trained_len`), see include/specdec.h."""
+    theta: float
+    rotary_dim: int
+    layout: str = "half"
+    scaling: str = "none"
+    factor: float = 1.0
+    low: float = 1.0
+    high: float = 4.0
+    trained_len: int = 8192
+    magnitude: float = 1.0
+
+    def _c(self) -> _Rope:
+        return _Rope(self.theta, self.rotary_dim, {"half": 0, "interleaved": 1}[self.layout],
+                     {"none": 0, "linear": 1, "by_parts": 2}[self.scaling], self.factor, self.low, self.high, self.trained_len,
+                     self.magnitude)
 
 
 class Model:
@@ -175,6 +215,10 @@ class Model:
         of the two); the two agree within the parity tolerance, not bit for bit."""
         _check(lib().sd_set_fused(self.handle, 1 if on else 0))
 
+    def set_rope(self, rope: Rope):
+        """sd_set_rope: the model's steps with scaled positions, from the current stream on (call it before the first prompt)."""
+        _check(lib().sd_set_rope(self.handle, C.byref(rope._c()), _stream()))
+
     def set_layer_timeline(self, buf: torch.Tensor | None):
         """Diagnostic time stamps of the layer kernel into an int64 CUDA tensor [launches, 24, 256] (None: off)."""
         if buf is None:
@@ -206,17 +250,20 @@ class Model:
 class KVCache:
     """sd_kv_*: the cache buffer is a torch allocation; its tiling is private to the library."""
 
-    def __init__(self, model: Model, batch: int, cap: int, buf: torch.Tensor | None = None):
+    def __init__(self, model: Model, batch: int, cap: int, buf: torch.Tensor | None = None, rows: str = "model"):
         """`buf`: a uint8 CUDA tensor of at least sd_kv_bytes bytes to hold the cache (its old contents do
-        not matter: sd_kv_create clears it); allocated here when None."""
+        not matter: sd_kv_create clears it); allocated here when None. `rows`: "model", the model's element type, or "e4m3",
+        8 bits with one exponent per head and 32 rows (sd_kv8_create; bfloat16 models)."""
         self.model, self.batch, self.cap = model, batch, cap
-        nbytes = lib().sd_kv_bytes(C.byref(model.cfg), batch, cap)
+        size, create = {"model": (lib().sd_kv_bytes, lib().sd_kv_create), "e4m3": (lib().sd_kv8_bytes, lib().sd_kv8_create)}[rows]
+        self.rows = rows
+        nbytes = size(C.byref(model.cfg), batch, cap)
         if buf is None:
             buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device="cuda")
         assert buf.is_cuda and buf.dtype == torch.uint8 and buf.is_contiguous() and buf.numel() >= nbytes
         self.buf = buf
         self.handle = C.c_void_p()
-        _check(lib().sd_kv_create(model.handle, batch, cap, self.buf.data_ptr(), nbytes, C.byref(self.handle)))
+        _check(create(model.handle, batch, cap, self.buf.data_ptr(), nbytes, C.byref(self.handle)))
 
     def len(self) -> list[int]:
         out = (C.c_int32 * self.batch)()
@@ -239,6 +286,36 @@ class KVCache:
         v = torch.empty_like(k)
         _check(lib().sd_kv_read_rows(self.handle, layer, seq, row0, nrows, k.data_ptr(), v.data_ptr(), _stream()))
         return k, v
+
+    def write_layers(self, seq, row0, k_rows, v_rows):
+        """sd_kv_write_layers: rows [n_layers, n, n_heads, head_dim] of every layer."""
+        s = self.model.shape
+        assert k_rows.dtype == v_rows.dtype == self.model.torch_dtype and k_rows.is_cuda and v_rows.is_cuda
+        assert k_rows.is_contiguous() and v_rows.is_contiguous() and k_rows.shape == v_rows.shape
+        assert k_rows.dim() == 4 and (k_rows.shape[0], *k_rows.shape[2:]) == (s.n_layers, s.n_heads, s.head_dim)
+        _check(lib().sd_kv_write_layers(self.handle, seq, row0, k_rows.shape[1], k_rows.data_ptr(), v_rows.data_ptr(), _stream()))
+
+    def read_layers(self, seq, row0, nrows, out=None):
+        """sd_kv_read_layers: (k, v), each [n_layers, nrows, n_heads, head_dim]; `out`: two such tensors to read into."""
+        s = self.model.shape
+        shape = (s.n_layers, nrows, s.n_heads, s.head_dim)
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=self.model.torch_dtype, device="cuda") for _ in range(2))
+        k, v = out
+        assert k.shape == v.shape == shape and k.dtype == v.dtype == self.model.torch_dtype and k.is_cuda and v.is_cuda
+        assert k.is_contiguous() and v.is_contiguous()
+        _check(lib().sd_kv_read_layers(self.handle, seq, row0, nrows, k.data_ptr(), v.data_ptr(), _stream()))
+        return k, v
+
+    def fork(self, seq: int, dst: "KVCache", dst_seqs):
+        """sd_kv_fork: the rows, length and draft state of `seq` copied into the sequences `dst_seqs` of `dst` (or of this cache)."""
+        to = [int(b) for b in dst_seqs]
+        _check(lib().sd_kv_fork(self.handle, seq, dst.handle, _i32_array(to), len(to), _stream()))
+
+    def drop_rows(self, seq: int, ranges):
+        """sd_kv_drop_rows: `ranges` = ascending (first, count) pairs of rows to drop; the rows behind move up, their keys rotated."""
+        first, count = [r[0] for r in ranges], [r[1] for r in ranges]
+        _check(lib().sd_kv_drop_rows(self.handle, seq, _i32_array(first), _i32_array(count), len(first), _stream()))
 
     def set_draft(self, root_tok, cand):
         """Root token and candidates of every sequence, from the current stream on; the call does not wait. int32 tensors on the
@@ -370,6 +447,49 @@ def kv_commit_rows(model: Model, kv: KVCache, src_slots: torch.Tensor, n_rows: t
     assert src_slots.shape[0] == kv.batch and n_rows.numel() == kv.batch
     _check(lib().sd_kv_commit_rows(model.handle, kv.handle, src_slots.data_ptr(), n_rows.data_ptr(), src_slots.shape[1],
                                    _stream()))
+
+
+def _row_distance(t: torch.Tensor) -> int:
+    """Elements between the rows of [batch, T, heads, dim] whose heads are contiguous and whose rows lie evenly."""
+    B, T, nh, hd = t.shape
+    assert t.is_cuda and t.stride(3) == 1 and (nh == 1 or t.stride(2) == hd)
+    ld = t.stride(1) if T > 1 else t.stride(0) if B > 1 else nh * hd
+    assert B == 1 or t.stride(0) == T * ld
+    return ld
+
+
+def tree_attention(model: Model, kv: KVCache, tree: Tree, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """sd_tree_attention: the attention stage over a cache in 8 bits. q, k, v: bfloat16 CUDA [batch, T, n_heads, head_dim], rotated;
+    they may be parts of one packed projection (rows the same distance apart in all three)."""
+    s = model.shape
+    want = (kv.batch, tree.T, s.n_heads, s.head_dim)
+    assert q.shape == k.shape == v.shape == want and q.dtype == k.dtype == v.dtype == torch.bfloat16
+    if out is None:
+        out = torch.empty(want, dtype=torch.bfloat16, device="cuda")
+    assert out.shape == want and out.dtype == torch.bfloat16
+    ld = _row_distance(q)
+    assert _row_distance(k) == ld and _row_distance(v) == ld
+    _check(lib().sd_tree_attention(model.handle, kv.handle, tree.handle, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), ld,
+                                   out.data_ptr(), _row_distance(out), _stream()))
+    return out
+
+
+def rope_rows(x: torch.Tensor, pos: torch.Tensor, rope: Rope, *, inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """sd_rope_rows: bfloat16 or float32 CUDA rows [n, heads, dim] (heads contiguous, rows any distance apart) rotated to the int32
+    positions `pos` [n]; `out` may be x. inverse: the gradient."""
+    assert x.is_cuda and x.dim() == 3 and x.dtype in (torch.bfloat16, torch.float32)
+    n, nh, hd = x.shape
+    assert pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n
+    if out is None:
+        out = torch.empty((n, nh, hd), dtype=x.dtype, device="cuda")
+    assert out.is_cuda and out.shape == x.shape and out.dtype == x.dtype
+    for t in (x, out):
+        assert n == 0 or (t.stride(2) == 1 and (nh == 1 or t.stride(1) == hd))
+    ld = [t.stride(0) if n > 1 else nh * hd for t in (x, out)]
+    _check(lib().sd_rope_rows(C.byref(rope._c()), 1 if x.dtype == torch.bfloat16 else 0, x.data_ptr(), ld[0], out.data_ptr(), ld[1],
+                              pos.data_ptr(), n, nh, hd, 1 if inverse else 0, _stream()))
+    return out
 
 
 def verify_tree(tree: Tree, tok: torch.Tensor, am: torch.Tensor, stop_mask: torch.Tensor, vocab: int,

@@ -10,6 +10,9 @@
 
 #include "sd_internal.h"
 #include "attn_geom.h"
+#include "attn8.h"
+#include "kv_seq.h"
+#include "rope.h"
 
 // ------------------------------------------------------------------------------------------ errors
 static thread_local char g_err[512] = "";
@@ -87,7 +90,7 @@ struct sd_model {
     void* xh;                                // draft-head rows of every tree row, in 256-row operand chunks
     int draft_schedule = SD_DRAFT_AFTER_ACCEPT;
     RowTable rt;
-    double* rope_freq;                       // [head_dim / 2]
+    double* rope_freq;                       // [head_dim / 2 + 1], see launch_rope_freqs
     PassMap* rm_dev;                         // the row map of a prompt pass, in device memory
     int prompt_rows = 0;                     // rows of the largest prompt pass; above 256 its plans and buffers exist:
     KwPlan kw[2][3];                         // 16, 32 rows; QKV, O, down projection
@@ -157,6 +160,9 @@ struct sd_kv {
     size_t layer_stride;                     // elements between layers, per K or V plane
     uint16_t *kc, *vc;                       // plane bases
     float *kc32 = nullptr, *vc32 = nullptr;  // float32 models: planes [layer][seq][cap][d], layer_stride = B * cap * d
+    bool q8 = false;                         // rows in 8 bits (kv8.h): all layers of c8 instead of kc, vc
+    Kv8 c8 = {};
+    DropState* drop = nullptr;               // device: scratch of sd_kv_drop_rows
     int32_t* state = nullptr;                // device: kv_len, n_old, root_tok, last_row, cand, io scratch
     int32_t *kv_len, *n_old, *root_tok, *last_row, *cand, *i_nacc, *i_tokens, *i_slots;
     std::vector<int32_t> len_hi;             // host upper bound of the committed lengths
@@ -250,7 +256,7 @@ static int create_f32(const sd_config* cfg, const sd_weights* w, int max_rows, h
     const size_t w_cs = wtake((size_t)Mp * (hd / 2) * 8), w_g = wtake(3 * 4), w_fin = wtake(SD_MAX_BATCH * 4);
     const size_t w_best = wtake((size_t)std::max(Mp, SD_MAX_BATCH) * rank_chunks(V) * 8);
     const size_t w_rk = wtake((size_t)std::min(H * SD_MAX_BATCH, 256) * rank_chunks(V) * cfg->topk * 8);
-    const size_t w_rm = wtake(sizeof(PassMap)), w_freq = wtake((size_t)(hd / 2) * 8);
+    const size_t w_rm = wtake(sizeof(PassMap)), w_freq = wtake((size_t)(hd / 2 + 1) * 8);
     const size_t w_rs = wtake((size_t)Mp * 16), w_zs = wtake((size_t)ceil_div(V, 32) * 4);
     if (e == hipSuccess) e = hipMalloc((void**)&m->work, wz);
     if (e == hipSuccess) e = hipMemsetAsync(m->work, 0, wz, s);
@@ -453,7 +459,7 @@ extern "C" int sd_model_create(const sd_config* cfg, const sd_weights* w, int32_
     size_t w_cs = wtake((size_t)Mr * (hd / 2) * 8), w_g = wtake(3 * 4), w_fin = wtake(SD_MAX_BATCH * 4);
     size_t w_best = wtake((size_t)std::max(Mp, SD_MAX_BATCH) * rank_chunks(V) * 8);
     size_t w_rk = wtake((size_t)std::min(H * SD_MAX_BATCH, 256) * rank_chunks(V) * cfg->topk * 8);
-    size_t w_rs = wtake((size_t)Mp * 16), w_rm = wtake(sizeof(PassMap)), w_freq = wtake((size_t)(hd / 2) * 8);
+    size_t w_rs = wtake((size_t)Mp * 16), w_rm = wtake(sizeof(PassMap)), w_freq = wtake((size_t)(hd / 2 + 1) * 8);
     size_t w_xh = wtake(align_up((size_t)H * Mp, 256) * d * 4);
     size_t w_zs = wtake((size_t)ceil_div(V, 32) * 4), w_zf = wtake(2048);
     size_t w_ssqa = wtake((size_t)align_up(d / 16, 4) * Mp * 4), w_ssqf = wtake((size_t)align_up(d / 16, 4) * Mp * 4);
@@ -666,13 +672,17 @@ extern "C" size_t sd_kv_bytes(const sd_config* cfg, int32_t batch, int32_t cap) 
     return (size_t)cfg->n_layers * 2 * batch * cfg->n_heads * blocks * 32 * cfg->head_dim * 2;
 }
 
-extern "C" int sd_kv_create(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, sd_kv** out) {
-    if (!m || !dev_buf || !out) return fail(SD_ERR_NULL, "sd_kv_create: NULL argument");
-    *out = nullptr;
+extern "C" size_t sd_kv8_bytes(const sd_config* cfg, int32_t batch, int32_t cap) {
+    if (!cfg || batch < 1 || cap < 1 || cfg->dtype != SD_DTYPE_BF16) return 0;
+    return (size_t)cfg->n_layers * batch * cfg->n_heads * ceil_div(cap, 32) * (2 * 32 * cfg->head_dim + 2);   // codes, exponents
+}
+
+static int create_kv(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, bool q8, sd_kv** out) {
+    const size_t need = q8 ? sd_kv8_bytes(&m->cfg, batch, cap) : sd_kv_bytes(&m->cfg, batch, cap);
     if (batch < 1 || batch > SD_MAX_BATCH) return fail(SD_ERR_SHAPE, "batch must be in 1..%d", SD_MAX_BATCH);
     if (batch * m->cfg.n_medusa > 256) return fail(SD_ERR_SHAPE, "batch * n_medusa must be <= 256");
     if (cap < m->cfg.n_medusa + 2) return fail(SD_ERR_SHAPE, "cap too small");
-    if (bytes < sd_kv_bytes(&m->cfg, batch, cap)) return fail(SD_ERR_SHAPE, "KV buffer too small");
+    if (bytes < need) return fail(SD_ERR_SHAPE, "KV buffer too small");
     if (((uintptr_t)dev_buf) & 15) return fail(SD_ERR_SHAPE, "KV buffer must be 16-byte aligned");
     sd_kv* kv = new (std::nothrow) sd_kv();
     if (!kv) return fail(SD_ERR_HIP, "out of host memory");
@@ -689,16 +699,23 @@ extern "C" int sd_kv_create(const sd_model* m, int32_t batch, int32_t cap, void*
         kv->kc32 = (float*)dev_buf;
         kv->vc32 = kv->kc32 + (size_t)m->cfg.n_layers * kv->layer_stride;
     }
+    if (q8) {
+        kv->q8 = true;
+        const size_t blocks = (size_t)batch * m->cfg.n_heads * kv->cap_blocks, plane = blocks * 32 * m->cfg.head_dim;
+        kv->c8 = Kv8{(uint8_t*)dev_buf, (uint8_t*)dev_buf + m->cfg.n_layers * plane, (int8_t*)dev_buf + 2 * m->cfg.n_layers * plane,
+                     kv->cap_blocks, plane, blocks * 2};
+    }
     const int H = m->cfg.n_medusa, k = m->cfg.topk;
     const int W = std::max(H + 1, SD_MAX_TREE);
-    size_t n = (size_t)batch * (4 + H * k + 1 + 2 * W);
-    hipError_t e = hipMalloc((void**)&kv->state, n * 4);
+    const size_t n = (size_t)batch * (4 + H * k + 1 + 2 * W), n_state = align_up(n * 4, 256) + sizeof(DropState);
+    hipError_t e = hipMalloc((void**)&kv->state, n_state);
     if (e != hipSuccess) { delete kv; return fail(SD_ERR_HIP, "hipMalloc state: %s", hipGetErrorString(e)); }
-    e = hipMemset(kv->state, 0, n * 4);
+    kv->drop = (DropState*)((char*)kv->state + align_up(n * 4, 256));
+    e = hipMemset(kv->state, 0, n_state);
     // The cache itself starts as zeros: attention multiplies the value rows of a partly filled block by
     // probabilities that are exactly 0 for the rows past the committed length, and 0 * NaN is NaN, so no
     // row the kernels can touch may hold a non-finite bit pattern left behind by the buffer's last user.
-    if (e == hipSuccess) e = hipMemset(dev_buf, 0, sd_kv_bytes(&m->cfg, batch, cap));
+    if (e == hipSuccess) e = hipMemset(dev_buf, 0, need);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) { hipFree(kv->state); delete kv; return fail(SD_ERR_HIP, "hipMemset: %s", hipGetErrorString(e)); }
     int32_t* p = kv->state;
@@ -713,6 +730,18 @@ extern "C" int sd_kv_create(const sd_model* m, int32_t batch, int32_t cap, void*
     kv->len_hi.assign(batch, 0);
     *out = kv;
     return SD_OK;
+}
+
+extern "C" int sd_kv_create(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, sd_kv** out) {
+    if (!m || !dev_buf || !out) return fail(SD_ERR_NULL, "sd_kv_create: NULL argument");
+    *out = nullptr;
+    return create_kv(m, batch, cap, dev_buf, bytes, false, out);
+}
+extern "C" int sd_kv8_create(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, sd_kv** out) {
+    if (!m || !dev_buf || !out) return fail(SD_ERR_NULL, "sd_kv8_create: NULL argument");
+    *out = nullptr;
+    if (m->f32) return fail(SD_ERR_SHAPE, "sd_kv8_create: rows in 8 bits need a bfloat16 model");
+    return create_kv(m, batch, cap, dev_buf, bytes, true, out);
 }
 
 extern "C" int sd_kv_destroy(sd_kv* kv) {
@@ -745,17 +774,28 @@ extern "C" int sd_kv_set_len(sd_kv* kv, const int32_t* len, void* stream) {
     return SD_OK;
 }
 
+static Kv8 kv8_layer(const sd_kv* kv, int layer) {
+    Kv8 c = kv->c8;
+    c.k += layer * c.code_stride; c.v += layer * c.code_stride; c.ex += layer * c.ex_stride;
+    return c;
+}
+
 static int kv_rows_common(sd_kv* kv, int layer, int seq, int row0, int nrows, void* k_rows, void* v_rows, int to_cache,
                           void* stream) {
-    if (!kv || !k_rows || !v_rows) return fail(SD_ERR_NULL, "sd_kv_*_rows: NULL argument");
+    if (!kv || (nrows != 0 && (!k_rows || !v_rows))) return fail(SD_ERR_NULL, "sd_kv_*_rows: NULL argument");
     const sd_config& c = kv->m->cfg;
-    if (layer < 0 || layer >= c.n_layers || seq < 0 || seq >= kv->B || row0 < 0 || nrows < 0 || row0 + nrows > kv->cap)
+    if (layer < 0 || layer >= c.n_layers || seq < 0 || seq >= kv->B || row0 < 0 || nrows < 0 || (int64_t)row0 + nrows > kv->cap)
         return fail(SD_ERR_SHAPE, "sd_kv_*_rows: index out of range");
-    if (nrows == 0) return SD_OK;
+    if (nrows == 0) return SD_OK;                      // (an empty array has no address)
     if (kv->m->f32) {
         const size_t o = layer * kv->layer_stride + (size_t)seq * kv->cap * c.d_model;
         launch_f32_kv_rows(kv->kc32 + o, kv->vc32 + o, (float*)k_rows, (float*)v_rows, row0, nrows, c.d_model, to_cache,
                            (hipStream_t)stream);
+        HIP_TRY(hipGetLastError());
+        return SD_OK;
+    }
+    if (kv->q8) {
+        launch_kv8_rows(kv8_layer(kv, layer), k_rows, v_rows, row0, nrows, c.n_heads, c.head_dim, seq, 1, to_cache, (hipStream_t)stream);
         HIP_TRY(hipGetLastError());
         return SD_OK;
     }
@@ -786,6 +826,171 @@ extern "C" int sd_kv_get_draft(sd_kv* kv, int32_t* root_tok, int32_t* cand, void
     if (!kv || !root_tok || !cand) return fail(SD_ERR_NULL, "sd_kv_get_draft: NULL argument");
     const sd_config& c = kv->m->cfg;
     launch_copy_i32(kv->root_tok, root_tok, kv->B, kv->cand, cand, kv->B * c.n_medusa * c.topk, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return SD_OK;
+}
+
+// Rows of every layer at once, [layer][row][head][dim].
+static int kv_layers_common(sd_kv* kv, int seq, int row0, int nrows, void* k_rows, void* v_rows, int to_cache, void* stream, const char* who) {
+    if (!kv || (nrows != 0 && (!k_rows || !v_rows))) return fail(SD_ERR_NULL, "%s: NULL argument", who);
+    const sd_config& c = kv->m->cfg;
+    if (seq < 0 || seq >= kv->B || row0 < 0 || nrows < 0 || (int64_t)row0 + nrows > kv->cap) return fail(SD_ERR_SHAPE, "%s: index out of range", who);
+    if (nrows == 0) return SD_OK;
+    if (kv->q8) {
+        launch_kv8_rows(kv->c8, k_rows, v_rows, row0, nrows, c.n_heads, c.head_dim, seq, c.n_layers, to_cache, (hipStream_t)stream);
+        HIP_TRY(hipGetLastError());
+        return SD_OK;
+    }
+    const size_t layer = (size_t)nrows * c.d_model * (kv->m->f32 ? 4 : 2);
+    for (int l = 0; l < c.n_layers; ++l)
+        if (int rc = kv_rows_common(kv, l, seq, row0, nrows, (char*)k_rows + l * layer, (char*)v_rows + l * layer, to_cache, stream)) return rc;
+    return SD_OK;
+}
+extern "C" int sd_kv_write_layers(sd_kv* kv, int32_t seq, int32_t row0, int32_t nrows, const void* k_rows, const void* v_rows, void* stream) {
+    return kv_layers_common(kv, seq, row0, nrows, (void*)k_rows, (void*)v_rows, 1, stream, "sd_kv_write_layers");
+}
+extern "C" int sd_kv_read_layers(sd_kv* kv, int32_t seq, int32_t row0, int32_t nrows, void* k_rows, void* v_rows, void* stream) {
+    return kv_layers_common(kv, seq, row0, nrows, k_rows, v_rows, 0, stream, "sd_kv_read_layers");
+}
+
+// Calls that move the host's bounds on the lengths: a replay would move the device's lengths behind them.
+static int refuse_capture(void* stream, const char* who) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing((hipStream_t)stream, &cap));
+    if (cap != hipStreamCaptureStatusNone) return fail(SD_ERR_STATE, "%s: the stream is being captured", who);
+    return SD_OK;
+}
+
+static KvPlanes planes_of(const sd_kv* kv) {
+    const sd_config& c = kv->m->cfg;
+    KvPlanes p = {};
+    if (kv->m->f32) {
+        p.p[0] = (char*)kv->kc32; p.p[1] = (char*)kv->vc32;
+        p.layer = kv->layer_stride * 4; p.head = (size_t)kv->cap * c.d_model * 4;
+        p.unit_rows = 1; p.unit_bytes = c.d_model * 4;
+    } else if (kv->q8) {
+        p.p[0] = (char*)kv->c8.k; p.p[1] = (char*)kv->c8.v; p.ex = (char*)kv->c8.ex;
+        p.layer = kv->c8.code_stride; p.head = (size_t)kv->cap_blocks * 32 * c.head_dim;
+        p.ex_layer = kv->c8.ex_stride; p.ex_head = (size_t)kv->cap_blocks * 2;
+        p.unit_rows = 32; p.unit_bytes = 32 * c.head_dim;
+    } else {
+        p.p[0] = (char*)kv->kc; p.p[1] = (char*)kv->vc;
+        p.layer = kv->layer_stride * 2; p.head = (size_t)kv->cap_blocks * 32 * c.head_dim * 2;
+        p.unit_rows = 32; p.unit_bytes = 32 * c.head_dim * 2;
+    }
+    return p;
+}
+
+extern "C" int sd_kv_fork(sd_kv* src, int32_t src_seq, sd_kv* dst, const int32_t* dst_seqs, int32_t n_dst, void* stream) {
+    if (!src || !dst || !dst_seqs) return fail(SD_ERR_NULL, "sd_kv_fork: NULL argument");
+    if (src->m != dst->m) return fail(SD_ERR_STATE, "sd_kv_fork: the caches belong to different models");
+    if (src->q8 != dst->q8) return fail(SD_ERR_SHAPE, "sd_kv_fork: one cache holds its rows in 8 bits, the other does not");
+    if (src_seq < 0 || src_seq >= src->B) return fail(SD_ERR_SHAPE, "sd_kv_fork: sequence %d out of range", src_seq);
+    if (n_dst < 1 || n_dst > dst->B) return fail(SD_ERR_SHAPE, "sd_kv_fork: n_dst must be in 1..%d", dst->B);
+    SeqList to = {};
+    for (int i = 0; i < n_dst; ++i) {
+        const int b = dst_seqs[i];
+        if (b < 0 || b >= dst->B) return fail(SD_ERR_SHAPE, "sd_kv_fork: sequence %d out of range", b);
+        if (src == dst && b == src_seq) return fail(SD_ERR_SHAPE, "sd_kv_fork: sequence %d cannot be its own copy", b);
+        for (int j = 0; j < i; ++j)
+            if (dst_seqs[j] == b) return fail(SD_ERR_SHAPE, "sd_kv_fork: sequence %d is named twice", b);
+        to.seq[i] = b;
+    }
+    if (src->len_hi[src_seq] > dst->cap)
+        return fail(SD_ERR_KV_FULL, "sd_kv_fork: up to %d rows do not fit a capacity of %d", src->len_hi[src_seq], dst->cap);
+    if (int rc = refuse_capture(stream, "sd_kv_fork")) return rc;
+    const sd_config& c = src->m->cfg;
+    launch_kv_fork(planes_of(src), planes_of(dst), to, n_dst, src->kv_len, src_seq, src->len_hi[src_seq], src->m->f32 ? 1 : c.n_heads,
+                   c.n_layers, KvCarried{src->kv_len, src->root_tok, src->cand}, KvCarried{dst->kv_len, dst->root_tok, dst->cand},
+                   c.n_medusa * c.topk, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    for (int i = 0; i < n_dst; ++i) dst->len_hi[to.seq[i]] = src->len_hi[src_seq];
+    dst->has_draft = dst->has_draft || src->has_draft;
+    return SD_OK;
+}
+
+extern "C" int sd_kv_drop_rows(sd_kv* kv, int32_t seq, const int32_t* first, const int32_t* count, int32_t n_ranges, void* stream) {
+    if (!kv || !first || !count) return fail(SD_ERR_NULL, "sd_kv_drop_rows: NULL argument");
+    if (seq < 0 || seq >= kv->B) return fail(SD_ERR_SHAPE, "sd_kv_drop_rows: sequence %d out of range", seq);
+    if (n_ranges < 1 || n_ranges > SD_MAX_DROP_RANGES) return fail(SD_ERR_SHAPE, "sd_kv_drop_rows: n_ranges must be in 1..%d", SD_MAX_DROP_RANGES);
+    DropRanges r = {};
+    r.n = n_ranges;
+    const int hi = kv->len_hi[seq];
+    int gone = 0;                                      // of the longest that the sequence may be
+    for (int i = 0; i < n_ranges; ++i) {
+        if (first[i] < 0 || count[i] < 1 || (int64_t)first[i] + count[i] > kv->cap || (i && first[i] < first[i - 1] + count[i - 1]))
+            return fail(SD_ERR_SHAPE, "sd_kv_drop_rows: range %d must hold rows of the cache, behind the range before it", i);
+        r.first[i] = first[i];
+        r.count[i] = count[i];
+        gone += std::max(0, std::min(count[i], hi - first[i]));
+    }
+    if (int rc = refuse_capture(stream, "sd_kv_drop_rows")) return rc;
+    const sd_model* m = kv->m;
+    launch_kv_drop(m->f32 ? 0 : kv->q8 ? 2 : 1, planes_of(kv), seq, m->cfg.n_heads, m->cfg.head_dim, m->cfg.n_layers, r, m->rope_freq,
+                   kv->kv_len, hi, kv->drop, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    kv->len_hi[seq] = hi - gone;
+    return SD_OK;
+}
+
+// ------------------------------------------------------------------------------------------ rotary embedding
+// radians per position of every pair
+static int rope_table(const sd_rope* r, RopeTable* t, const char* who) {
+    if (!(r->theta > 0.f) || !std::isfinite(r->theta)) return fail(SD_ERR_SHAPE, "%s: bad theta", who);
+    if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > ROPE_MAX_DIM)
+        return fail(SD_ERR_SHAPE, "%s: rotary_dim must be even, in 2..%d", who, ROPE_MAX_DIM);
+    if (r->layout != SD_ROPE_HALF && r->layout != SD_ROPE_INTERLEAVED) return fail(SD_ERR_SHAPE, "%s: unknown layout %d", who, r->layout);
+    if (r->scaling < SD_ROPE_PLAIN || r->scaling > SD_ROPE_BY_PARTS) return fail(SD_ERR_SHAPE, "%s: unknown scaling %d", who, r->scaling);
+    if (!std::isfinite(r->magnitude) || !(r->magnitude > 0.f)) return fail(SD_ERR_SHAPE, "%s: magnitude must be positive and finite", who);
+    if (r->scaling != SD_ROPE_PLAIN && (!(r->factor > 0.f) || !std::isfinite(r->factor))) return fail(SD_ERR_SHAPE, "%s: bad factor", who);
+    if (r->scaling == SD_ROPE_BY_PARTS && (!(r->high > r->low) || !std::isfinite(r->low) || !std::isfinite(r->high) || r->trained_len < 1))
+        return fail(SD_ERR_SHAPE, "%s: by parts needs low < high and a trained length", who);
+    memset(t, 0, sizeof(*t));
+    t->rotary = r->rotary_dim;
+    t->magnitude = r->magnitude;
+    for (int i = 0; i < r->rotary_dim / 2; ++i) {
+        double f = std::pow((double)r->theta, -2.0 * i / r->rotary_dim);
+        if (r->scaling == SD_ROPE_LINEAR) f /= (double)r->factor;
+        if (r->scaling == SD_ROPE_BY_PARTS) {
+            const double turns = (double)r->trained_len * f / (2.0 * M_PI);
+            const double keep = std::min(1.0, std::max(0.0, (turns - (double)r->low) / ((double)r->high - (double)r->low)));
+            f *= keep + (1.0 - keep) / (double)r->factor;
+        }
+        t->turns[i] = f;
+    }
+    return SD_OK;
+}
+
+extern "C" int sd_rope_rows(const sd_rope* rope, int32_t dtype, const void* x, int64_t ld_x, void* y, int64_t ld_y, const int32_t* pos,
+                            int32_t n_rows, int32_t n_heads, int32_t head_dim, int32_t inverse, void* stream) {
+    if (!rope) return fail(SD_ERR_NULL, "sd_rope_rows: NULL argument");
+    RopeTable t;
+    if (int rc = rope_table(rope, &t, "sd_rope_rows")) return rc;
+    if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_ERR_SHAPE, "sd_rope_rows: dtype must be SD_DTYPE_BF16 or SD_DTYPE_F32");
+    if (n_rows < 0 || n_heads < 1 || n_heads > 1024 || head_dim < 2 || head_dim > 1024 || rope->rotary_dim > head_dim)
+        return fail(SD_ERR_SHAPE, "sd_rope_rows: bad sizes");
+    const int64_t row = (int64_t)n_heads * head_dim;
+    if (ld_x < row || ld_y < row) return fail(SD_ERR_SHAPE, "sd_rope_rows: rows overlap (ld < n_heads * head_dim)");
+    if (x == y && ld_x != ld_y) return fail(SD_ERR_SHAPE, "sd_rope_rows: in place needs one row distance");
+    if (n_rows == 0) return SD_OK;                     // the pointers are not looked at
+    if (!x || !y || !pos) return fail(SD_ERR_NULL, "sd_rope_rows: NULL argument");
+    const int size = dtype == SD_DTYPE_F32 ? 4 : 2;
+    if (((uintptr_t)x | (uintptr_t)y) % size) return fail(SD_ERR_SHAPE, "sd_rope_rows: rows must be aligned to their elements");
+    for (int i = 0; i < t.rotary / 2; ++i) t.turns[i] *= (inverse ? -1.0 : 1.0) / (2.0 * M_PI);
+    launch_rope_rows(x, y, pos, t, dtype == SD_DTYPE_F32, rope->layout == SD_ROPE_INTERLEAVED, n_rows, n_heads, head_dim, ld_x, ld_y,
+                     (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return SD_OK;
+}
+
+extern "C" int sd_set_rope(sd_model* m, const sd_rope* rope, void* stream) {
+    if (!m || !rope) return fail(SD_ERR_NULL, "sd_set_rope: NULL argument");
+    RopeTable t;
+    if (int rc = rope_table(rope, &t, "sd_set_rope")) return rc;
+    if (rope->layout != SD_ROPE_HALF || rope->rotary_dim != m->cfg.head_dim)
+        return fail(SD_ERR_SHAPE, "sd_set_rope: a model's steps rotate whole heads of %d dims in halves", m->cfg.head_dim);
+    if (int rc = refuse_capture(stream, "sd_set_rope")) return rc;
+    launch_set_rope(t, m->rope_freq, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return SD_OK;
 }
@@ -937,23 +1142,35 @@ static bool have_plans(const sd_model* m, int M, int B, bool heads, bool all_row
 }
 
 // Does a pass over M rows run through the persistent layer kernel?
-static bool fused_eligible(const sd_model* m, int M) {
-    if (m->f32) return false;
+static bool fused_eligible(const sd_model* m, const sd_kv* kv, int M) {
+    if (m->f32 || kv->q8) return false;
     const int MB = pow2_blocks(M);
     return m->use_fused && m->fused_ok && (MB == 1 || MB == 2 || MB == 8);
 }
 // The geometry that the pass over B sequences of Tp rows will launch: worked out once per pass, launched, and part of the
 // key under which the pass is captured. (float32 attention has no parts: none of its launches depends on n_hi.)
 struct PassGeom : AttnGeom { AttnSplit split; int whole; };     // whole: 0, or the parts of attn_whole.hip (1: none)
+// (k_attn_merge counts the parts of sequences that differ in four bits each)
+static AttnSplit split_of_8(const sd_model* m, int B, int Tp, const int* len) {
+    const int TB = Tp / 32, TBW = attn8_tbw(TB);
+    return attn8_split(m->cfg.n_heads * ceil_div(TB, TBW), attn8_resident(TB), B, TB, len, B > 1 ? 15 : m->max_parts);
+}
 // M: the pass's rows (a short prompt has fewer than its padded B * Tp).
 static PassGeom pass_geometry(const sd_model* m, const sd_kv* kv, const int32_t* seq, int B, int M, int Tp, int n_hi) {
     PassGeom g = {};
     if (m->f32) return g;
+    if (kv->q8) {
+        int len[SD_MAX_BATCH];
+        for (int i = 0; i < B; ++i) len[i] = kv->len_hi[seq ? seq[i] : i];
+        g.split = split_of_8(m, B, Tp, len);
+        g.ncparts = g.nparts = g.split.max_parts;
+        return g;
+    }
     // (a batch is cut sequence by sequence once its longest one has 256 rows)
-    static_cast<AttnGeom&>(g) = attn_geometry_of_pass(fused_eligible(m, B * Tp), m->cfg.n_heads, m->max_parts, B, Tp, n_hi,
+    static_cast<AttnGeom&>(g) = attn_geometry_of_pass(fused_eligible(m, kv, B * Tp), m->cfg.n_heads, m->max_parts, B, Tp, n_hi,
                                                       B > 1 && n_hi >= 256);
     // (a handful of rows take the merged parts as an operand of another layout)
-    g.whole = !fused_eligible(m, B * Tp) && !few_layers(m, M) ? attn_whole_parts(m->cfg.n_heads, B, Tp, n_hi) : 0;
+    g.whole = !fused_eligible(m, kv, B * Tp) && !few_layers(m, M) ? attn_whole_parts(m->cfg.n_heads, B, Tp, n_hi) : 0;
     if (g.whole > 1) g.nparts = g.whole;
     if (g.per == 0) {
         int len[SD_MAX_BATCH];
@@ -1008,13 +1225,19 @@ static PartView run_layers(sd_model* m, sd_kv* kv, RowRef rr, const RowMap& rm, 
         // the launch saved is worth more than it costs (batch of eight 32-node trees: attention 65.4 -> 72.8 us, the
         // 11.8 us launch gone, step -0.8 %); so it is with the parts of a batch that is cut sequence by sequence, the last of
         // which takes the tree.
-        const AttnSplit* split = ag.split.n ? &ag.split : nullptr;
-        const bool fr = Tp <= 64 && (ag.whole || ag.tree_sep || ag.ncparts == 1 || split);
+        const AttnSplit* split = ag.split.n && !(kv->q8 && B == 1) ? &ag.split : nullptr;      // (NULL: nparts everywhere)
+        const bool fr = !kv->q8 && Tp <= 64 && (ag.whole || ag.tree_sep || ag.ncparts == 1 || split);
         if (!fr) launch_rope_kv(pq, m->rt, rr, m->q, kt, vt, B, Tp, nh, hd, s);
         // algorithmic bytes: one read of K and V of the committed rows (upper bound n_hi) + tree rows
-        const int pa = prof_claim(m, PROF_ATTN, (double)B * (n_hi + Tp) * 2.0 * d * 2.0);
+        const int pa = prof_claim(m, PROF_ATTN, (double)B * (n_hi * (kv->q8 ? 0.5 : 1.0) + Tp) * 2.0 * d * 2.0);
         const uint16_t *kc = kv->kc + l * kv->layer_stride, *vc = kv->vc + l * kv->layer_stride;
-        if (ag.whole)
+        if (kv->q8) {
+            Attn8 a = {};
+            a.c = kv8_layer(kv, l); a.kv_len = kv->kv_len; a.rr = rr; a.B = B; a.nh = nh; a.hd = hd; a.Tp = Tp; a.split = ag.split;
+            a.opart = m->opart; a.mlpart = m->mlpart;
+            a.qp = (const bf16x8*)m->q; a.kt = (const bf16x8*)kt; a.vt = (const bf16x8*)vt; a.anc = m->rt.anc;
+            launch_attn8(a, s, prof_ev(m, pa, 0), prof_ev(m, pa, 1));
+        } else if (ag.whole)
             launch_attn_whole(m->q, kc, vc, kt, vt, kv->kv_len, m->rt.anc, m->attn_x, rr, B, nh, hd, Tp, kv->cap_blocks, MB, s,
                               prof_ev(m, pa, 0), prof_ev(m, pa, 1), fr ? &pq : nullptr, fr ? &m->rt : nullptr, ag.whole, m->opart, m->mlpart);
         else
@@ -1146,6 +1369,8 @@ static void commit_rows(sd_model* m, sd_kv* kv, const ScratchRows& sc, bool by_s
     if (m->f32)
         launch_f32_kv_commit(m->f.kt, m->f.vt, kv->kc32, kv->vc32, slots, n_acc, kv->n_old, rm, sc.row0, kv->B, c.n_layers, sc.n,
                              c.d_model, sc.M, kv->cap, W, s);
+    else if (kv->q8)
+        launch_kv8_commit(m->kt, m->vt, kv->c8, slots, n_acc, kv->n_old, rm, c.n_layers, sc.n, c.n_heads, c.head_dim, sc.Tp / 32, W, s);
     else
         launch_kv_commit(m->kt, m->vt, kv->kc, kv->vc, slots, n_acc, kv->n_old, rm, kv->B, c.n_layers, sc.n, c.n_heads,
                          c.head_dim, sc.Tp / 32, kv->cap_blocks, W, s);
@@ -1208,7 +1433,7 @@ static PartView run_forward(sd_model* m, sd_kv* kv, const RowMap& rm, int B, int
                             bool want_lm, bool keep_h, hipStream_t s) {
     const RowRef rr = {R ? nullptr : m->rm_dev, R};
     if (m->f32) { run_forward_f32(m, kv, rr, rm, B, M, Tp, want_lm, s); return dense_logits(m, m->logits); }
-    if (fused_eligible(m, B * Tp)) {
+    if (fused_eligible(m, kv, B * Tp)) {
         // (when the final norm's rows themselves are wanted, the last stage runs as kernels of its own)
         PartView pl = run_forward_fused(m, kv, rr, B, Tp, n_hi, ag, want_lm && !keep_h, s);
         return want_lm && keep_h ? run_lm_head(m, pl, M, s, true) : pl;
@@ -1348,9 +1573,10 @@ static std::vector<PromptChunk> joined_chunks(const PromptPass* passes, int n, b
 }
 
 // Which passes run as one: as many as its buffers hold, where that is the sooner done.
-static std::vector<int> join_passes(const sd_model* m, const std::vector<PromptPass>& passes) {
+// (Not over a cache in 8 bits: a block's codes hang on all of its rows, so chunks that share one are committed one after the other.)
+static std::vector<int> join_passes(const sd_model* m, const sd_kv* kv, const std::vector<PromptPass>& passes) {
     const int n = (int)passes.size();
-    if (m->prompt_rows <= 256 || fused_eligible(m, 256)) return std::vector<int>(n, 1);
+    if (m->prompt_rows <= 256 || kv->q8 || fused_eligible(m, kv, 256)) return std::vector<int>(n, 1);
     return prompt_runs(
         n,
         [&](int i, int k) {
@@ -1393,7 +1619,7 @@ static void run_prompt_pass(sd_model* m, sd_kv* kv, const int32_t* tokens, const
     memset(&fin, 0, sizeof(fin));
     memset(&last, 0, sizeof(last));
     int M = 0, n_hi = 0;
-    const bool padded = fused_eligible(m, A * Tp);         // that pass takes the rows as [sequence][Tp]
+    const bool padded = fused_eligible(m, kv, A * Tp);         // that pass takes the rows as [sequence][Tp]
     for (int i = 0; i < A; ++i) {
         const PromptChunk& ch = p.chunks[i];
         ca.len[i] = ch.len;
@@ -1522,7 +1748,7 @@ extern "C" int sd_prefill(sd_model* m, sd_kv* kv, const int32_t* tokens, const i
             return fail(SD_ERR_STATE, "sd_prefill: no launch plan for %d rows (internal inconsistency)", rows);
     const std::vector<PromptPass> passes = cut_prompts(m, lens, B);
     size_t i = 0;
-    for (int k : join_passes(m, passes)) {
+    for (int k : join_passes(m, kv, passes)) {
         if (k > 1) run_prompt_passes(m, kv, tokens, &passes[i], k, i + k == passes.size(), s);
         else run_prompt_pass(m, kv, tokens, passes[i], s);
         i += k;
@@ -1554,7 +1780,7 @@ static int step_common(sd_model* m, sd_kv* kv, uint64_t tree_uid, const int32_t*
     const bool heads = T > 1 || m->greedy_drafts;      // plain greedy decoding may leave the draft heads out
     // rows of a sequence lie R apart: the tree's own nodes, no padding (see RowMap), except where the pass takes them
     // as [sequence][Tp]
-    const int R = fused_eligible(m, B * Tp) ? Tp : T, M = B * R;
+    const int R = fused_eligible(m, kv, B * Tp) ? Tp : T, M = B * R;
     RowMap rm;
     memset(&rm, 0, sizeof(rm));
     for (int b = 0; b < B; ++b) { rm.off[b] = b * R; rm.len[b] = R; rm.seq[b] = b; }
@@ -1575,7 +1801,7 @@ static int step_common(sd_model* m, sd_kv* kv, uint64_t tree_uid, const int32_t*
     float* lg = io->logits && dense ? io->logits : (io->logits || ty) ? m->logits : nullptr;
     const int ldl = lg == m->logits ? m->Vpad : c.vocab;
     // plain decoding drafts from the only row a sequence has: one pass of the LM head for its base and head rows
-    const bool known = T == 1 && dense && heads && !fused_eligible(m, B * Tp);
+    const bool known = T == 1 && dense && heads && !fused_eligible(m, kv, B * Tp);
     PartView pl = run_forward(m, kv, rm, B, M, R, Tp, n_hi, ag, !known, all_rows, s);
     if (known) {
         run_known_rows(m, kv, pl, B, nullptr, every_sequence(), lg, ldl, io->head_logits, s);
@@ -1729,6 +1955,30 @@ extern "C" int sd_verify_tree(const sd_tree* tree, int32_t batch, int32_t n_medu
     va.tok = tok; va.am = am; va.stop_mask = stop_mask;
     va.n_accept = n_accept; va.n_accept_raw = n_accept_raw; va.tokens = tokens; va.src_slots = src_slots;
     launch_verify(va, batch, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return SD_OK;
+}
+
+extern "C" int sd_tree_attention(sd_model* m, sd_kv* kv, const sd_tree* tree, int32_t layer, const void* q, const void* k, const void* v,
+                                 int32_t ld, void* out, int32_t ld_out, void* stream) {
+    if (!m || !kv || !tree || !q || !k || !v || !out) return fail(SD_ERR_NULL, "sd_tree_attention: NULL argument");
+    if (kv->m != m) return fail(SD_ERR_STATE, "sd_tree_attention: cache belongs to another model");
+    if (!kv->q8) return fail(SD_ERR_SHAPE, "sd_tree_attention: the cache must hold its rows in 8 bits (sd_kv8_create)");
+    const sd_config& c = m->cfg;
+    if (layer < 0 || layer >= c.n_layers) return fail(SD_ERR_SHAPE, "sd_tree_attention: layer %d out of range", layer);
+    if (ld < c.d_model || ld_out < c.d_model || ld % 8 || ld_out % 8)
+        return fail(SD_ERR_SHAPE, "sd_tree_attention: row distances must be multiples of 8, at least d_model");
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15)
+        return fail(SD_ERR_SHAPE, "sd_tree_attention: rows must be 16-byte aligned");
+    if (pow2_blocks(kv->B * tree->Tp) > m->MBmax) return fail(SD_ERR_SHAPE, "sd_tree_attention: %d rows exceed the model's max_rows", kv->B * tree->Tp);
+    Attn8 a = {};
+    a.c = kv8_layer(kv, layer); a.kv_len = kv->kv_len; a.rr = RowRef{nullptr, tree->T}; a.B = kv->B; a.nh = c.n_heads; a.hd = c.head_dim;
+    a.Tp = tree->Tp;
+    a.split = split_of_8(m, kv->B, tree->Tp, kv->len_hi.data());
+    a.opart = m->opart; a.mlpart = m->mlpart;
+    a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.ld = ld; a.T = tree->T; a.parent = tree->parent;
+    a.out = (uint16_t*)out; a.ldo = ld_out;
+    launch_attn8(a, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return SD_OK;
 }

@@ -142,3 +142,35 @@ static inline int attn_whole_parts(int n_heads, int B, int Tp, int n_hi) {
 // tokens of the 7B shape 3348 / 3388, 4096 6831 / 7263. Few heads ask for no line of their own: 4, 8 and 16 heads, prompts of 300 to 1000 tokens
 // and batches of two to eight in chunks of 32 to 256 rows take 0.92 to 0.99 of the time; eight prompts of 33 tokens, chunks of 32 rows, 0.96 to 1.005.
 static inline bool attn_whole_pays_prompt(int Tp, int n_hi) { return (n_hi + 31) / 32 + Tp / 32 <= 32; }
+
+// ---- caches in 8 bits (attn8.hip)
+// Parts of every sequence: one entry per (sequence, part), each a workgroup per head and group of query blocks. Parts share a
+// sequence's items (its cache blocks, then its tree blocks) evenly, as many as the device says there are. groups: heads x query
+// groups, resident: workgroups that the chip holds at once, most: parts of one sequence that the partials have room for.
+// Two items per wave before another part is opened: every part fetches the queries and adds a term to the merge.
+static inline AttnSplit attn8_split(int groups, int resident, int B, int TB, const int* len, int most) {
+    AttnSplit s = {};
+    int want = resident / groups, longest = 0;
+    if (want > ATTN_SPLIT_MAX) want = ATTN_SPLIT_MAX;
+    for (int b = 0; b < B; ++b) longest = len[b] > longest ? len[b] : longest;
+    auto items = [&](int b) { return (len[b] + 31) / 32 + TB; };
+    auto parts = [&](int b, int q) {
+        const int p = (items(b) + q - 1) / q;
+        return p < 1 ? 1 : p > most ? most : p;
+    };
+    int q = 8;
+    for (;; ++q) {                                     // (bounded: at the longest sequence's items everything has one part)
+        int total = 0;
+        for (int b = 0; b < B; ++b) total += parts(b, q);
+        if (total <= want || q >= (longest + 31) / 32 + TB) break;
+    }
+    for (int b = 0; b < B; ++b) {
+        const int n = parts(b, q);
+        if (n > s.max_parts) s.max_parts = n;
+        for (int p = 0; p < n && s.n < ATTN_SPLIT_MAX; ++p) s.slot[s.n++] = (uint32_t)b | (uint32_t)p << 8 | (uint32_t)n << 16;
+    }
+    return s;
+}
+// Query blocks per workgroup, and the workgroups of it that a compute unit holds
+static inline int attn8_tbw(int TB) { return TB >= 2 ? 2 : 1; }
+static inline int attn8_resident(int TB) { return attn8_tbw(TB) == 2 ? 256 : 512; }

@@ -8,17 +8,19 @@
 // ------------------------------------------------------------------------------------------
 // Rotary angles in float64, so that positions up to ~17k lose nothing. The frequencies theta^(-2i/hd) are a table of the
 // model's (pow() in float64 for every row and dim was most of the row-building launch).
+// Behind them lies the factor of every cosine and sine, 1 unless sd_set_rope says otherwise.
 __global__ void k_rope_freqs(double* __restrict__ freq, int hd, float theta) {
     const int i = threadIdx.x;
     if (i < hd / 2) freq[i] = pow((double)theta, -2.0 * (double)i / (double)hd);
+    else if (i == hd / 2) freq[i] = 1.0;
 }
 void launch_rope_freqs(double* freq, int hd, float theta, hipStream_t s) {
     hipLaunchKernelGGL(k_rope_freqs, dim3(1), dim3(128), 0, s, freq, hd, theta);
 }
-static __device__ inline float2 rope_cs(int pos, double freq) {
+static __device__ inline float2 rope_cs(int pos, double freq, double magnitude) {
     double s, c;
     sincos((double)pos * freq, &s, &c);
-    return make_float2((float)c, (float)s);
+    return make_float2((float)(c * magnitude), (float)(s * magnitude));
 }
 
 // (embed_f32: the table holds float32 instead of bfloat16) 16 bytes per thread and load; d is a multiple of 32
@@ -71,7 +73,7 @@ __global__ void k_build_rows_tree(RowTable rt, const int32_t* __restrict__ paren
         rt.tok[m] = tok;
         rt.pos[m] = pos;
     }
-    for (int i = threadIdx.x; i < hd / 2; i += blockDim.x) rt.cs[(size_t)m * (hd / 2) + i] = rope_cs(pos, freq[i]);
+    for (int i = threadIdx.x; i < hd / 2; i += blockDim.x) rt.cs[(size_t)m * (hd / 2) + i] = rope_cs(pos, freq[i], freq[hd / 2]);
     embed_row(embed, embed_f32, tok, d, x + (size_t)m * d, valid);
 }
 
@@ -116,7 +118,7 @@ __global__ void k_build_rows_chain(RowTable rt, const int32_t* __restrict__ toke
         rt.tok[m] = tok;
         rt.pos[m] = pos;
     }
-    for (int i = threadIdx.x; i < hd / 2; i += blockDim.x) rt.cs[(size_t)m * (hd / 2) + i] = rope_cs(pos, freq[i]);
+    for (int i = threadIdx.x; i < hd / 2; i += blockDim.x) rt.cs[(size_t)m * (hd / 2) + i] = rope_cs(pos, freq[i], freq[hd / 2]);
     embed_row(embed, embed_f32, tok, d, x + (size_t)m * d, valid);
 }
 

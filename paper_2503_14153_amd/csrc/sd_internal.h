@@ -280,7 +280,7 @@ int fused_max_resident(int device);
 void launch_reduce_selected(PartView pv, float* dst, const int32_t* sel, int B, int H, int M, int row0, int rows,
                             hipStream_t s);
 
-// freq [head_dim / 2]: rotary frequencies
+// freq [head_dim / 2 + 1]: rotary frequencies, and the factor of the cosines and sines
 void launch_rope_freqs(double* freq, int hd, float theta, hipStream_t s);
 void launch_build_rows_tree(RowTable rt, const int32_t* parent, const int32_t* depth, const int32_t* rank,
                             const int32_t* root_tok, const int32_t* cand, const int32_t* kv_len,
