@@ -101,6 +101,7 @@ struct sd_model {
     float2* best; void* ranked;                 // ranking scratch: arg-max per row and chunk, top-k per head row and chunk
     float4* row_stats;                     // [Mp]: per tree row, statistics for typical acceptance
     uint32_t* zero_stop;
+    int32_t* arrived;                        // [rows / 32][head], zeros between launches: see k_attn8
     const void* zfrag;                       // 2 KiB of zeros
     size_t part_floats;
     int max_parts;
@@ -172,8 +173,9 @@ struct sd_kv {
 struct sd_tree {
     uint64_t uid = next_uid();
     int T, Tp, H, topk;
-    int32_t* dev = nullptr;                  // parent | depth | rank
+    int32_t* dev = nullptr;                  // ancestor sets | parent | depth | rank
     const int32_t *parent, *depth, *rank;
+    const uint32_t* anc;                     // [Tp][SD_ANC_WORDS]: bit i of row j: i is j or an ancestor of it (none past T)
 };
 
 // ------------------------------------------------------------------------------------------ model
@@ -464,6 +466,7 @@ extern "C" int sd_model_create(const sd_config* cfg, const sd_weights* w, int32_
     size_t w_zs = wtake((size_t)ceil_div(V, 32) * 4), w_zf = wtake(2048);
     size_t w_ssqa = wtake((size_t)align_up(d / 16, 4) * Mp * 4), w_ssqf = wtake((size_t)align_up(d / 16, 4) * Mp * 4);
     size_t w_xn2 = wtake((size_t)Mp * d * 4);
+    size_t w_arr = wtake((size_t)m->MBmax * nh * 4);
     // the persistent layer kernel: partial sums of each of its four GEMMs in a buffer of their own, a second
     // packed operand, and the barrier counters of every launch of a pass
     int dev_now = 0;
@@ -512,6 +515,7 @@ extern "C" int sd_model_create(const sd_config* cfg, const sd_weights* w, int32_
     m->rm_dev = (PassMap*)(Wk + w_rm);
     m->row_stats = (float4*)(Wk + w_rs);
     m->g_parent = (int32_t*)(Wk + w_g); m->g_depth = m->g_parent + 1; m->g_rank = m->g_parent + 2;
+    m->arrived = (int32_t*)(Wk + w_arr);
     m->zero_stop = (uint32_t*)(Wk + w_zs);
     m->zfrag = Wk + w_zf;
     m->ssq_a = (float*)(Wk + w_ssqa); m->ssq_f = (float*)(Wk + w_ssqf);
@@ -674,7 +678,8 @@ extern "C" size_t sd_kv_bytes(const sd_config* cfg, int32_t batch, int32_t cap) 
 
 extern "C" size_t sd_kv8_bytes(const sd_config* cfg, int32_t batch, int32_t cap) {
     if (!cfg || batch < 1 || cap < 1 || cfg->dtype != SD_DTYPE_BF16) return 0;
-    return (size_t)cfg->n_layers * batch * cfg->n_heads * ceil_div(cap, 32) * (2 * 32 * cfg->head_dim + 2);   // codes, exponents
+    const int blocks = ceil_div(cap, 32);
+    return (size_t)cfg->n_layers * batch * cfg->n_heads * ((size_t)blocks * 2 * 32 * cfg->head_dim + kv8_ex_head(blocks));
 }
 
 static int create_kv(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, bool q8, sd_kv** out) {
@@ -701,9 +706,9 @@ static int create_kv(const sd_model* m, int32_t batch, int32_t cap, void* dev_bu
     }
     if (q8) {
         kv->q8 = true;
-        const size_t blocks = (size_t)batch * m->cfg.n_heads * kv->cap_blocks, plane = blocks * 32 * m->cfg.head_dim;
+        const size_t heads = (size_t)batch * m->cfg.n_heads, plane = heads * kv->cap_blocks * 32 * m->cfg.head_dim;
         kv->c8 = Kv8{(uint8_t*)dev_buf, (uint8_t*)dev_buf + m->cfg.n_layers * plane, (int8_t*)dev_buf + 2 * m->cfg.n_layers * plane,
-                     kv->cap_blocks, plane, blocks * 2};
+                     kv->cap_blocks, plane, heads * kv8_ex_head(kv->cap_blocks)};
     }
     const int H = m->cfg.n_medusa, k = m->cfg.topk;
     const int W = std::max(H + 1, SD_MAX_TREE);
@@ -871,7 +876,7 @@ static KvPlanes planes_of(const sd_kv* kv) {
     } else if (kv->q8) {
         p.p[0] = (char*)kv->c8.k; p.p[1] = (char*)kv->c8.v; p.ex = (char*)kv->c8.ex;
         p.layer = kv->c8.code_stride; p.head = (size_t)kv->cap_blocks * 32 * c.head_dim;
-        p.ex_layer = kv->c8.ex_stride; p.ex_head = (size_t)kv->cap_blocks * 2;
+        p.ex_layer = kv->c8.ex_stride; p.ex_head = kv8_ex_head(kv->cap_blocks);
         p.unit_rows = 32; p.unit_bytes = 32 * c.head_dim;
     } else {
         p.p[0] = (char*)kv->kc; p.p[1] = (char*)kv->vc;
@@ -1024,18 +1029,24 @@ extern "C" int sd_tree_create(int32_t T, const int32_t* parent, const int32_t* d
     t->Tp = ceil_div(T, 32) * 32;
     t->H = n_medusa;
     t->topk = topk;
-    hipError_t e = hipMalloc((void**)&t->dev, (size_t)3 * T * 4);
-    if (e == hipSuccess) e = hipMemcpy(t->dev, parent, (size_t)T * 4, hipMemcpyHostToDevice);
-    if (e == hipSuccess) e = hipMemcpy(t->dev + T, depth, (size_t)T * 4, hipMemcpyHostToDevice);
-    if (e == hipSuccess) e = hipMemcpy(t->dev + 2 * T, rank, (size_t)T * 4, hipMemcpyHostToDevice);
+    const size_t words = (size_t)t->Tp * SD_ANC_WORDS;
+    std::vector<int32_t> host(words + (size_t)3 * T, 0);
+    for (int j = 0; j < T; ++j)
+        for (int i = j; i >= 0; i = parent[i]) host[(size_t)j * SD_ANC_WORDS + (i >> 5)] |= (int32_t)(1u << (i & 31));
+    std::copy(parent, parent + T, host.begin() + words);
+    std::copy(depth, depth + T, host.begin() + words + T);
+    std::copy(rank, rank + T, host.begin() + words + 2 * T);
+    hipError_t e = hipMalloc((void**)&t->dev, host.size() * 4);
+    if (e == hipSuccess) e = hipMemcpy(t->dev, host.data(), host.size() * 4, hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         if (t->dev) hipFree(t->dev);
         delete t;
         return fail(SD_ERR_HIP, "tree upload: %s", hipGetErrorString(e));
     }
-    t->parent = t->dev;
-    t->depth = t->dev + T;
-    t->rank = t->dev + 2 * T;
+    t->anc = (const uint32_t*)t->dev;
+    t->parent = t->dev + words;
+    t->depth = t->parent + T;
+    t->rank = t->parent + 2 * T;
     *out = t;
     return SD_OK;
 }
@@ -1149,11 +1160,11 @@ static bool fused_eligible(const sd_model* m, const sd_kv* kv, int M) {
 }
 // The geometry that the pass over B sequences of Tp rows will launch: worked out once per pass, launched, and part of the
 // key under which the pass is captured. (float32 attention has no parts: none of its launches depends on n_hi.)
-struct PassGeom : AttnGeom { AttnSplit split; int whole; };     // whole: 0, or the parts of attn_whole.hip (1: none)
+struct PassGeom : AttnGeom { AttnSplit split; int whole; Attn8Split eight; };     // whole: 0, or the parts of attn_whole.hip (1: none)
 // (k_attn_merge counts the parts of sequences that differ in four bits each)
-static AttnSplit split_of_8(const sd_model* m, int B, int Tp, const int* len) {
-    const int TB = Tp / 32, TBW = attn8_tbw(TB);
-    return attn8_split(m->cfg.n_heads * ceil_div(TB, TBW), attn8_resident(TB), B, TB, len, B > 1 ? 15 : m->max_parts);
+static Attn8Split split_of_8(const sd_model* m, int B, int Tp, const int* len) {
+    const int TB = Tp / 32;
+    return attn8_split(m->cfg.n_heads * ceil_div(TB, attn8_query_blocks(TB)), attn8_resident(TB), B, TB, len, B > 1 ? 15 : m->max_parts);
 }
 // M: the pass's rows (a short prompt has fewer than its padded B * Tp).
 static PassGeom pass_geometry(const sd_model* m, const sd_kv* kv, const int32_t* seq, int B, int M, int Tp, int n_hi) {
@@ -1162,7 +1173,8 @@ static PassGeom pass_geometry(const sd_model* m, const sd_kv* kv, const int32_t*
     if (kv->q8) {
         int len[SD_MAX_BATCH];
         for (int i = 0; i < B; ++i) len[i] = kv->len_hi[seq ? seq[i] : i];
-        g.split = split_of_8(m, B, Tp, len);
+        g.eight = split_of_8(m, B, Tp, len);
+        g.split = g.eight;                             // (whose parts the merge joins)
         g.ncparts = g.nparts = g.split.max_parts;
         return g;
     }
@@ -1233,7 +1245,7 @@ static PartView run_layers(sd_model* m, sd_kv* kv, RowRef rr, const RowMap& rm, 
         const uint16_t *kc = kv->kc + l * kv->layer_stride, *vc = kv->vc + l * kv->layer_stride;
         if (kv->q8) {
             Attn8 a = {};
-            a.c = kv8_layer(kv, l); a.kv_len = kv->kv_len; a.rr = rr; a.B = B; a.nh = nh; a.hd = hd; a.Tp = Tp; a.split = ag.split;
+            a.c = kv8_layer(kv, l); a.kv_len = kv->kv_len; a.rr = rr; a.B = B; a.nh = nh; a.hd = hd; a.Tp = Tp; a.split = ag.eight;
             a.opart = m->opart; a.mlpart = m->mlpart;
             a.qp = (const bf16x8*)m->q; a.kt = (const bf16x8*)kt; a.vt = (const bf16x8*)vt; a.anc = m->rt.anc;
             launch_attn8(a, s, prof_ev(m, pa, 0), prof_ev(m, pa, 1));
@@ -1849,6 +1861,8 @@ static int step_common(sd_model* m, sd_kv* kv, uint64_t tree_uid, const int32_t*
                                      (uint64_t)(m->use_fused ? 1 : 0) | ((uint64_t)m->sync_timeout_ticks << 1),
                                      (uint64_t)(uintptr_t)m->timeline, (uint64_t)m->timeline_launches};
         key.insert(key.end(), ag.split.slot, ag.split.slot + ag.split.n);
+        key.insert(key.end(), ag.eight.each, ag.eight.each + ag.eight.n);
+        key.insert(key.end(), ag.eight.share, ag.eight.share + ag.eight.n);
         hipGraphExec_t exec = nullptr;
         for (const sd_model::StepGraph& g : m->graphs)
             if (g.key == key) { exec = g.exec; break; }
@@ -1976,8 +1990,9 @@ extern "C" int sd_tree_attention(sd_model* m, sd_kv* kv, const sd_tree* tree, in
     a.Tp = tree->Tp;
     a.split = split_of_8(m, kv->B, tree->Tp, kv->len_hi.data());
     a.opart = m->opart; a.mlpart = m->mlpart;
-    a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.ld = ld; a.T = tree->T; a.parent = tree->parent;
+    a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.ld = ld; a.T = tree->T; a.anc = tree->anc;
     a.out = (uint16_t*)out; a.ldo = ld_out;
+    a.arrived = m->arrived;
     launch_attn8(a, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return SD_OK;

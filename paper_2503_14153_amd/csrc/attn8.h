@@ -8,16 +8,16 @@ struct Attn8 {
     const int32_t* kv_len;
     RowRef rr;
     int B, nh, hd, Tp;
-    AttnSplit split;
+    Attn8Split split;
     float* opart; float2* mlpart;        // [seq][head][split.max_parts][Tp][hd], as launch_attn_merge takes them
-    // inside a pass: queries, tree keys and values, and ancestors as the rotary stage leaves them
+    const uint32_t* anc;                 // ancestor sets [Tp][SD_ANC_WORDS] (inside a pass: of every sequence)
+    // inside a pass: queries, tree keys and values as the rotary stage leaves them
     const bf16x8 *qp, *kt, *vt;
-    const uint32_t* anc;
-    // or the stage alone: natural rows [seq][T] of bfloat16, `ld` apart, and the tree's parents
+    // or the stage alone: natural rows [seq][T] of bfloat16, `ld` apart
     const uint16_t *q, *k, *v;
     int ld, T;
-    const int32_t* parent;
     uint16_t* out; int ldo;
+    int32_t* arrived;                    // zeros, one per (seq, head, query group): see k_attn8
 };
 // natural rows: also merges the parts into `out`
 void launch_attn8(const Attn8& a, hipStream_t s, hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);

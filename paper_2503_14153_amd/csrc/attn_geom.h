@@ -144,18 +144,22 @@ static inline int attn_whole_parts(int n_heads, int B, int Tp, int n_hi) {
 static inline bool attn_whole_pays_prompt(int Tp, int n_hi) { return (n_hi + 31) / 32 + Tp / 32 <= 32; }
 
 // ---- caches in 8 bits (attn8.hip)
-// Parts of every sequence: one entry per (sequence, part), each a workgroup per head and group of query blocks. Parts share a
-// sequence's items (its cache blocks, then its tree blocks) evenly, as many as the device says there are. groups: heads x query
-// groups, resident: workgroups that the chip holds at once, most: parts of one sequence that the partials have room for.
-// Two items per wave before another part is opened: every part fetches the queries and adds a term to the merge.
-static inline AttnSplit attn8_split(int groups, int resident, int B, int TB, const int* len, int most) {
-    AttnSplit s = {};
+// Parts of every sequence: one entry per (sequence, part), each a workgroup per head and group of query blocks. The host's bounds
+// fix which cache blocks an entry's four waves (or pairs of waves) start at, so that they can be requested before the device's
+// length is known: part p owns blocks [p * each, (p + 1) * each), quarter q of it `share` of them from p * each + q * share on, the
+// last quarter all that are left; and the last part has no end but the length, so that a launch that is replayed for a longer
+// sequence is still whole. The last part also has the tree's blocks, which count as items when the parts are made.
+// groups: heads x query groups, resident: workgroups that the chip holds at once, most: parts of one sequence that the partials
+// have room for. Two items per wave before another part is opened: every part fetches the queries and adds a term to the merge.
+struct Attn8Split : AttnSplit { int32_t each[ATTN_SPLIT_MAX], share[ATTN_SPLIT_MAX]; uint8_t parts[32]; };     // parts: of sequence b
+static inline Attn8Split attn8_split(int groups, int resident, int B, int TB, const int* len, int most) {
+    Attn8Split s = {};
     int want = resident / groups, longest = 0;
     if (want > ATTN_SPLIT_MAX) want = ATTN_SPLIT_MAX;
     for (int b = 0; b < B; ++b) longest = len[b] > longest ? len[b] : longest;
-    auto items = [&](int b) { return (len[b] + 31) / 32 + TB; };
+    auto blocks = [&](int b) { return (len[b] + 31) / 32; };
     auto parts = [&](int b, int q) {
-        const int p = (items(b) + q - 1) / q;
+        const int p = (blocks(b) + TB + q - 1) / q;
         return p < 1 ? 1 : p > most ? most : p;
     };
     int q = 8;
@@ -165,12 +169,18 @@ static inline AttnSplit attn8_split(int groups, int resident, int B, int TB, con
         if (total <= want || q >= (longest + 31) / 32 + TB) break;
     }
     for (int b = 0; b < B; ++b) {
-        const int n = parts(b, q);
+        const int n = parts(b, q), each = (blocks(b) + TB + n - 1) / n;
         if (n > s.max_parts) s.max_parts = n;
-        for (int p = 0; p < n && s.n < ATTN_SPLIT_MAX; ++p) s.slot[s.n++] = (uint32_t)b | (uint32_t)p << 8 | (uint32_t)n << 16;
+        s.parts[b] = (uint8_t)n;
+        for (int p = 0; p < n && s.n < ATTN_SPLIT_MAX; ++p) {
+            const int left = blocks(b) - p * each, mine = left < 0 ? 0 : p == n - 1 || left < each ? left : each;
+            s.each[s.n] = each;
+            s.share[s.n] = (mine + 3) / 4;
+            s.slot[s.n++] = (uint32_t)b | (uint32_t)p << 8 | (uint32_t)n << 16;
+        }
     }
     return s;
 }
 // Query blocks per workgroup, and the workgroups of it that a compute unit holds
-static inline int attn8_tbw(int TB) { return TB >= 2 ? 2 : 1; }
-static inline int attn8_resident(int TB) { return attn8_tbw(TB) == 2 ? 256 : 512; }
+static inline int attn8_query_blocks(int TB) { return TB >= 2 ? 2 : 1; }
+static inline int attn8_resident(int TB) { return attn8_query_blocks(TB) == 2 ? 256 : 512; }

@@ -11,7 +11,7 @@
 // unit, so that a wave's load instruction fetches one contiguous KiB of a block:
 //   keys    K[i][lane][16]: row c, dim e: i = e/32, lane = c%32 + 32*((e/8)&1), byte 8*((e/16)&1) + e%8
 //   values  V[eb][lane][16]: row c, dim e: eb = e/32, lane = e%32 + 32*((c/4)&1), byte 8*((c%32)/16) + 4*((c/8)&1) + c%4
-// Exponents: two int8 per block (keys', values'), [layer][seq][head][block].
+// Exponents: two int8 per block (keys', values'), [layer][seq][head][block], a head's filled up to whole 4-byte words.
 #pragma once
 #include "sd_internal.h"
 
@@ -27,6 +27,8 @@ static __host__ __device__ inline size_t v8_index(int c, int e, int HD) {
 }
 // byte s of a value unit of lane half g is row v8_row(s, g) of its block
 static __host__ __device__ inline int v8_row(int s, int g) { return (s >> 3) * 16 + ((s >> 2) & 1) * 8 + 4 * g + (s & 3); }
+
+static __host__ __device__ inline size_t kv8_ex_head(int cap_blocks) { return (size_t)((cap_blocks + 1) / 2) * 4; }   // bytes
 
 // One layer of a cache in 8 bits, or (with the strides between layers) all of them.
 struct Kv8 {

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_kv8_rows(Kv8 c, uint16_t* __restrict__ 
     const size_t at = ((size_t)seq * nh + h) * c.cap_blocks + blk;
     uint8_t* kb = c.k + blockIdx.z * c.code_stride + at * (32 * HD);
     uint8_t* vb = c.v + blockIdx.z * c.code_stride + at * (32 * HD);
-    int8_t* ex = c.ex + blockIdx.z * c.ex_stride + at * 2;
+    int8_t* ex = c.ex + blockIdx.z * c.ex_stride + ((size_t)seq * nh + h) * kv8_ex_head(c.cap_blocks) + blk * 2;
     const int first = blk * 32 - row0;                 // natural row of the block's row 0 (negative: before the range)
     const size_t layer = (size_t)blockIdx.z * nrows;
     auto asked = [&](int r) { return first + r >= 0 && first + r < nrows; };
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void k_kv8_commit(const uint16_t* __restrict__
     const size_t at = ((size_t)rm.seq[b] * nh + h) * c.cap_blocks + blk;
     uint8_t* kb = c.k + l * c.code_stride + at * (32 * HD);
     uint8_t* vb = c.v + l * c.code_stride + at * (32 * HD);
-    int8_t* ex = c.ex + l * c.ex_stride + at * 2;
+    int8_t* ex = c.ex + l * c.ex_stride + ((size_t)rm.seq[b] * nh + h) * kv8_ex_head(c.cap_blocks) + blk * 2;
     const size_t src = l * layer_stride_t + ((size_t)b * nh + h) * TB * (32 * HD);
     auto fresh = [&](int r) { return r >= lo && r < hi; };
     auto slot = [&](int r) { return min(max(src_slots[(size_t)lst * W + r - lo], 0), last); };

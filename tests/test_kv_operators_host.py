@@ -27,9 +27,10 @@ def test_the_rope_structure_mirrors_the_header():
 
 
 def test_bytes_of_a_cache_in_8_bits(lib):  # noqa: F811
-    # layers * (K and V) * batch * heads * rows rounded up to blocks of 32 * head_dim, and two exponents per block and head
+    # layers * (K and V) * batch * heads * rows rounded up to blocks of 32 * head_dim, and two exponents per block and head (whole
+    # words of two blocks)
     assert lib.sd_kv8_bytes(C.byref(config()), 1, 2048) == 32 * 32 * (2 * 2048 * 128 + 64 * 2)
-    assert lib.sd_kv8_bytes(C.byref(config()), 8, 4097) == 32 * 8 * 32 * (2 * 4128 * 128 + 129 * 2)
+    assert lib.sd_kv8_bytes(C.byref(config()), 8, 4097) == 32 * 8 * 32 * (2 * 4128 * 128 + 130 * 2)
     assert lib.sd_kv8_bytes(None, 1, 16) == 0 and lib.sd_kv8_bytes(C.byref(config()), 0, 16) == 0
     assert lib.sd_kv8_bytes(C.byref(config(dtype=0)), 1, 16) == 0          # float32 models have no such cache
 
@@ -74,9 +75,9 @@ def test_bad_rows_are_refused(lib, dtype, ld_x, ld_y, n, heads, dim, x, y):  # n
 # ---------------------------------------------------------------------------------------------- parts of 8-bit attention
 CODE = """
 #include "attn_geom.h"
-extern "C" int split(int groups, int resident, int B, int TB, const int* len, int most, unsigned* slot, int* max_parts) {
-    AttnSplit s = attn8_split(groups, resident, B, TB, len, most);
-    for (int i = 0; i < s.n; ++i) slot[i] = s.slot[i];
+extern "C" int split(int groups, int resident, int B, int TB, const int* len, int most, unsigned* slot, int* each, int* share, int* max_parts) {
+    Attn8Split s = attn8_split(groups, resident, B, TB, len, most);
+    for (int i = 0; i < s.n; ++i) { slot[i] = s.slot[i]; each[i] = s.each[i]; share[i] = s.share[i]; }
     *max_parts = s.max_parts;
     return s.n;
 }
@@ -92,10 +93,10 @@ def split(tmp_path_factory):
     f = C.CDLL(str(d / "split.so")).split
 
     def call(groups, resident, TB, lens, most):
-        slot, parts = (C.c_uint * 64)(), C.c_int()
-        n = f(groups, resident, len(lens), TB, (C.c_int * len(lens))(*lens), most, slot, C.byref(parts))
+        slot, each, share, parts = (C.c_uint * 64)(), (C.c_int * 64)(), (C.c_int * 64)(), C.c_int()
+        n = f(groups, resident, len(lens), TB, (C.c_int * len(lens))(*lens), most, slot, each, share, C.byref(parts))
         assert 1 <= n <= 64
-        return [(s & 255, s >> 8 & 255, s >> 16) for s in slot[:n]], parts.value
+        return [(slot[i] & 255, slot[i] >> 8 & 255, slot[i] >> 16, each[i], share[i]) for i in range(n)], parts.value
     return call
 
 
@@ -103,16 +104,26 @@ def split(tmp_path_factory):
 @pytest.mark.parametrize("TB", [1, 2, 8])
 @pytest.mark.parametrize("lens", [[0], [1], [500], [16873], [10 ** 6], [0, 0, 0], [4096, 1024, 7, 0], [5] * 32, [17000] * 32,
                                   [0] * 31 + [16896]])
-def test_every_sequence_has_its_parts_once_and_they_share_its_blocks(split, groups, TB, lens):
+def test_every_sequence_has_its_parts_once_and_they_cover_its_blocks(split, groups, TB, lens):
     most = 15 if len(lens) > 1 else 65
     entries, max_parts = split(groups, 256 if TB > 1 else 512, TB, lens, most)
     assert max_parts == max(e[2] for e in entries) <= most
-    for b, n in enumerate(lens):
+    for b, bound in enumerate(lens):
         mine = [e for e in entries if e[0] == b]
         own = mine[0][2]
         assert [e[1] for e in mine] == list(range(own)) and all(e[2] == own for e in mine)
-        for ntree in range(1, TB + 1):                 # what the kernel makes of it, for every query group's tree blocks
-            total = (n + 31) // 32 + ntree
-            each = -(-total // own)
-            cut = [(min(p * each, total), min(min(p * each, total) + each, total)) for p in range(own)]
-            assert cut[0][0] == 0 and cut[-1][1] == total and all(a[1] == c[0] for a, c in zip(cut, cut[1:]))
+        # what the waves take of it, at lengths up to the bound and (a launch that is replayed) beyond it
+        for n in {0, 1, bound // 2, max(0, bound - 33), bound, bound + 40, 3 * bound + 1000}:
+            nblk, seen = (n + 31) // 32, 0
+            for _, part, _, each, share in mine:
+                end = nblk if part == own - 1 else min(nblk, (part + 1) * each)
+                for quarter in range(4):
+                    first = part * each + quarter * share
+                    last = end if quarter == 3 else min(end, first + share)
+                    if first < last:
+                        assert first == seen               # one after the other, nothing twice, nothing left out
+                        seen = last
+            assert seen == nblk
+        if bound:                                      # at the bound itself the waves have about the same
+            most_blocks = max(e[4] for e in mine)
+            assert most_blocks <= -(-(-(-(-(-bound // 32) + TB) // own)) // 4)
