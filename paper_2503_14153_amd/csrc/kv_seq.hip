@@ -63,16 +63,19 @@ void launch_kv_fork(const KvPlanes& src, const KvPlanes& dst, const SeqList& to,
 // of the format does not hang on how the products were taken; 4 multiply-adds per pair beside 2 loads and 2 stores do not count.
 //
 // Everything in place: dest rows 32 d .. of a block come from rows at or behind them, so a workgroup that walks the blocks of a
-// (layer, head, plane) in order reads every row before it is overwritten (a barrier between a block's reads and its writes). That
-// is one workgroup per (layer, head, plane): enough where a model has some thousand of them. Where it has fewer, `gridDim.x / nh`
-// workgroups share the blocks of [d0, d1), which the host makes no longer than the shortest shift: none of them then writes what
-// another one still has to read, and the launches follow one another.
+// (layer, head, plane) in order, G at a time, has read every row before it is overwritten (a barrier between the reads of G
+// blocks and their writes). That is one workgroup per (layer, head, plane): enough where a model has some thousand of them.
+// Where it has fewer, `gridDim.x / nh` workgroups share the blocks of [d0, d1), which the host makes no longer than the shortest
+// shift: none of them then writes what another one still has to read, and the launches follow one another.
+// G: a turn is a chain of memory round trips (exponents, rows, the barrier, the stores, some 5 us). Few walkers take four blocks a
+// turn; where workgroups fill the chip two, in as few registers as let several of them hide one another's chains.
+// d rounded to odd: cut to 24 bits, the last one set if anything was cut, so that a later rounding to fewer bits sees on which side
+// of a border d lies. (From the bits: below 29 bits of a float64's fraction, a float32's ends.)
 static __device__ __forceinline__ float odd_float(double d) {
-    const float f = (float)d;
-    if ((double)f == d) return f;
-    uint32_t b = __float_as_uint(f);
-    if (fabs((double)f) > fabs(d)) --b;
-    return __uint_as_float(b | 1u);
+    const uint64_t b = (uint64_t)__double_as_longlong(d);
+    const uint32_t lo = (uint32_t)b, cut = lo & 0x1fffffffu;
+    const uint32_t kept = (lo & 0xe0000000u) | ((cut + 0x1fffffffu) & 0x20000000u);
+    return (float)__longlong_as_double((long long)((b & 0xffffffff00000000ull) | kept));
 }
 static __device__ __forceinline__ int source_row(const DropRanges& R, int j, int& segment) {
     int s = j, i = 0;
@@ -97,25 +100,83 @@ __global__ void k_drop_setup(DropRanges R, const double* __restrict__ freq, int 
     }
 }
 
-// ST: 0 float32, 1 bfloat16, 2 e4m3
-template <int ST> struct Eight { float f[8]; };
+// ST: 0 float32, 1 bfloat16, 2 e4m3. Eight dims of a row as the first two store them.
+template <int ST> struct Raw { u32x4 a, b; };
+template <> struct Raw<1> { u16x8 a; };
 template <int ST, int HD>
-static __device__ __forceinline__ void load_row8(const char* p, int row, int e, int nh, float sc, float (&f)[8]) {
+static __device__ __forceinline__ Raw<ST> load_row8(const char* p, int row, int e, int nh) {
+    Raw<ST> r;
     if constexpr (ST == 0) {
-        const float4 a = *(const float4*)((const float*)p + (size_t)row * nh * HD + e), b = *(const float4*)((const float*)p + (size_t)row * nh * HD + e + 4);
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        r.a = *(const u32x4*)((const float*)p + (size_t)row * nh * HD + e);
+        r.b = *(const u32x4*)((const float*)p + (size_t)row * nh * HD + e + 4);
     } else if constexpr (ST == 1) {
-        const u16x8 v = *(const u16x8*)((const uint16_t*)p + kblk_index(row, e, HD));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = bf16_bits_to_float(v[i]);
-    } else {
-        const u32x2 q = *(const u32x2*)(p + k8_index(row, e, HD));
-        float a[4], b[4];
-        kv8_values(q.x, sc, a);
-        kv8_values(q.y, sc, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = a[i]; f[4 + i] = b[i]; }
+        r.a = *(const u16x8*)((const uint16_t*)p + kblk_index(row, e, HD));
     }
+    return r;
+}
+template <int ST>
+static __device__ __forceinline__ void row8_values(const Raw<ST>& r, float (&f)[8]) {
+    if constexpr (ST == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(r.a[i]); f[4 + i] = __uint_as_float(r.b[i]); }
+    } else if constexpr (ST == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = bf16_bits_to_float(r.a[i]);
+    }
+}
+template <int ST, int HD>
+static __device__ __forceinline__ void store_row8(char* p, int row, int e, int nh, const float (&f)[8]) {
+    if constexpr (ST == 0) {
+        *(float4*)((float*)p + (size_t)row * nh * HD + e) = make_float4(f[0], f[1], f[2], f[3]);
+        *(float4*)((float*)p + (size_t)row * nh * HD + e + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    } else if constexpr (ST == 1) {
+        u16x8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(uint16_t, (__bf16)f[i]);
+        *(u16x8*)((uint16_t*)p + kblk_index(row, e, HD)) = v;
+    }
+}
+// Eight pairs turned by the table's angles. A border between two numbers of a narrower format has its last 15 bits clear (bfloat16;
+// e4m3 19, of which 16 are looked at): where a float32 result has not, its own rounding decided nothing.
+template <int ST>
+static __device__ __forceinline__ void turn_pairs(const double2* __restrict__ table, float (&x)[8], float (&y)[8]) {
+    const uint32_t keep = ST == 1 ? 0x7fffu : 0xffffu;
+    uint16_t low = 0xffffu;
+    float u[8], v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const double2 w = table[k];
+        u[k] = (float)(x[k] * w.x - y[k] * w.y);
+        v[k] = (float)(x[k] * w.y + y[k] * w.x);
+        const uint16_t lu = (uint16_t)(__float_as_uint(u[k]) & keep), lv = (uint16_t)(__float_as_uint(v[k]) & keep);
+        low = low < lu ? low : lu;
+        low = low < lv ? low : lv;
+    }
+    if (ST != 0 && low == 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const double2 w = table[k];
+            u[k] = odd_float(x[k] * w.x - y[k] * w.y);
+            v[k] = odd_float(x[k] * w.y + y[k] * w.x);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { x[k] = u[k]; y[k] = v[k]; }
+}
+// Values that come from codes are finite or NaN, and a maximum of floats takes no NaN: the plain instruction does.
+static __device__ __forceinline__ float larger(float m, float a, float b) { return fmaxf(fmaxf(m, fabsf(a)), fabsf(b)); }
+// and those that had a say in their block's exponent need no clamp (kv8_four)
+static __device__ __forceinline__ uint32_t four_codes(const float (&f)[4], float scale) {
+    typedef __attribute__((ext_vector_type(2))) short s16x2;
+    s16x2 q = {0, 0};
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[0], f[1], scale, false);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[2], f[3], scale, true);
+    return __builtin_bit_cast(uint32_t, q);
+}
+static __device__ __forceinline__ void four_values(uint32_t codes, float scale, float (&f)[4]) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+    f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
 }
 template <int ST, int HD>
 static __device__ __forceinline__ void store_row8(char* p, int row, int e, int nh, float inv, const float (&f)[8]) {
@@ -130,23 +191,44 @@ static __device__ __forceinline__ void store_row8(char* p, int row, int e, int n
     } else {
         const float a[4] = {f[0], f[1], f[2], f[3]}, b[4] = {f[4], f[5], f[6], f[7]};
         u32x2 q;
-        q.x = kv8_four(a, inv);
-        q.y = kv8_four(b, inv);
+        q.x = four_codes(a, inv);
+        q.y = four_codes(b, inv);
         *(u32x2*)(p + k8_index(row, e, HD)) = q;
     }
 }
-static __device__ __forceinline__ uint32_t finite_bits(float f) {
-    const uint32_t a = __float_as_uint(f) & 0x7fffffffu;
-    return a < 0x7f800000u ? a : 0u;
+// The largest of the workgroup's magnitudes for each of G blocks -> exponents. One barrier, which also ends the reads of
+// those blocks. `most` alternates between turns: the one before it may still be read.
+template <int G>
+static __device__ __forceinline__ void exponents_of(float (&m)[G], float (*most)[4], int (&e)[G]) {
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+#pragma unroll
+        for (int o = 32; o; o >>= 1) m[i] = fmaxf(m[i], __shfl_xor(m[i], o));
+        if ((threadIdx.x & 63) == 0) most[i][threadIdx.x >> 6] = m[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < G; ++i) e[i] = kv8_exponent(fmaxf(fmaxf(most[i][0], most[i][1]), fmaxf(most[i][2], most[i][3])));
 }
 
-template <int ST, int HD>
-__global__ __launch_bounds__(256) void k_kv_drop(KvPlanes c, int seq, int nh, DropRanges R, const DropState* __restrict__ st, int d0, int d1) {
+// Do the rows of every block of [d, end) come from neighbouring rows? (The same answer in every thread.)
+static __device__ __forceinline__ bool one_shift(const DropRanges& R, int d, int end, int left) {
+    for (int b = d; b < end; ++b) {
+        int s;
+        const int j = b * 32, j1 = min(j + 31, left - 1);
+        if (source_row(R, j1, s) - source_row(R, j, s) != j1 - j) return false;
+    }
+    return true;
+}
+
+template <int ST, int HD, int G>
+__global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int seq, int nh, DropRanges R, const DropState* __restrict__ st, int d0, int d1) {
     constexpr int A = HD / 16;                         // pieces of 8 dims + their rotary partners per row
     constexpr int TW = 32 * A;                         // threads that have one
-    __shared__ uint32_t most[2][4];
-    __shared__ __attribute__((aligned(16))) uint16_t tile[32][HD + 8];
-    const int h = blockIdx.x % nh, lanes = gridDim.x / nh, plane = blockIdx.z, tid = threadIdx.x;
+    constexpr bool TILES = ST != 0;                    // values are stored turned: several rows of one dim to a piece
+    __shared__ float most[2][G][4];
+    __shared__ __attribute__((aligned(16))) uint16_t tile[TILES ? G : 1][32][HD + 8];
+    const int h = blockIdx.x % nh, walkers = gridDim.x / nh, plane = blockIdx.z, tid = threadIdx.x;
     const int len = st->old_len, left = st->new_len;
     if (left == len) return;                           // nothing of it is in the ranges
     const int end = min(d1, (left + 31) >> 5);
@@ -154,128 +236,262 @@ __global__ __launch_bounds__(256) void k_kv_drop(KvPlanes c, int seq, int nh, Dr
     char* p = c.p[plane] + blockIdx.y * c.layer + ((size_t)seq * heads + (ST == 0 ? 0 : h)) * c.head + (ST == 0 ? (size_t)h * HD * 4 : 0);
     int8_t* ex = ST == 2 ? (int8_t*)(c.ex + blockIdx.y * c.ex_layer + ((size_t)seq * nh + h) * c.ex_head) + plane : nullptr;
     int turn = 0;
-    for (int d = d0 + (int)blockIdx.x / nh; d < end; d += lanes, turn ^= 1) {
-        const bool natural = plane == 0 || ST == 0;    // rows as pieces of dims
-        float lo[8], hi[8];
-        uint32_t m = 0;
-        const int r = tid & 31, a = tid >> 5, j = d * 32 + r;
-        if (natural) {
-            const bool live = tid < TW && j < left;
+    for (int d = d0 + ((int)blockIdx.x / nh) * G; d < end; d += walkers * G, turn ^= 1) {
+        float m[G] = {};
+        int e[G] = {};
+        if (ST != 2 && (plane == 0 || !TILES)) {       // rows as pieces of dims
+            const int r = tid & 31, a = tid >> 5;
+            Raw<ST> lo[G], hi[G];
+            int seg[G];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { lo[i] = 0.f; hi[i] = 0.f; }
-            if (live) {
-                int seg;
-                const int s = source_row(R, j, seg);
-                const float sc = ST == 2 ? kv8_scale(ex[2 * (s >> 5)]) : 1.f;
-                load_row8<ST, HD>(p, s, a * 8, nh, sc, lo);
-                load_row8<ST, HD>(p, s, HD / 2 + a * 8, nh, sc, hi);
-                if (plane == 0 && seg) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const double2 w = st->table[seg - 1][a * 8 + i];
-                        const double x = lo[i], y = hi[i], u = x * w.x - y * w.y, v = x * w.y + y * w.x;
-                        lo[i] = ST == 0 ? (float)u : odd_float(u);
-                        hi[i] = ST == 0 ? (float)v : odd_float(v);
-                    }
+            for (int i = 0; i < G; ++i) {
+                const int j = (d + i) * 32 + r;
+                seg[i] = -1;
+                if (tid < TW && d + i < end && j < left) {
+                    const int s = source_row(R, j, seg[i]);
+                    lo[i] = load_row8<ST, HD>(p, s, a * 8, nh);
+                    hi[i] = load_row8<ST, HD>(p, s, HD / 2 + a * 8, nh);
                 }
             }
+            float f[G][16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, max(finite_bits(lo[i]), finite_bits(hi[i])));
-        } else {
-            // values: a stored piece holds one dim of several rows, so the block is put together in LDS, segment by segment
-            __syncthreads();                           // the tile's last readers are done
-            for (int r0 = 0; r0 < 32 && d * 32 + r0 < left;) {
+            for (int i = 0; i < G; ++i) {
+                float x[8], y[8];
+                if (seg[i] >= 0) {
+                    row8_values<ST>(lo[i], x);
+                    row8_values<ST>(hi[i], y);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) { x[k] = 0.f; y[k] = 0.f; }
+                }
+                if (plane == 0 && seg[i] > 0) turn_pairs<ST>(st->table[seg[i] - 1] + a * 8, x, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    f[i][k] = x[k];
+                    f[i][8 + k] = y[k];
+                }
+            }
+            __syncthreads();                           // every row of these blocks has been read
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int j = (d + i) * 32 + r;
+                if (tid < TW && d + i < end && j < left) {
+                    const float x[8] = {f[i][0], f[i][1], f[i][2], f[i][3], f[i][4], f[i][5], f[i][6], f[i][7]};
+                    const float y[8] = {f[i][8], f[i][9], f[i][10], f[i][11], f[i][12], f[i][13], f[i][14], f[i][15]};
+                    store_row8<ST, HD>(p, j, a * 8, nh, x);
+                    store_row8<ST, HD>(p, j, HD / 2 + a * 8, nh, y);
+                }
+            }
+        } else if (ST == 2 && plane == 0) {
+            // Keys: thread = one row of one block and two 16-byte units of it, sixteen dims and their rotary partners: a wave reads and
+            // writes whole runs of 512 bytes. (With eight dims to a thread, half units, the launch wrote 2.5 times its bytes.)
+            constexpr int NB = 256 / HD < G ? 256 / HD : G, ROUNDS = G / NB;
+            const int r = tid & 31, at = (((tid % HD) >> 6) * 64 + r + 32 * (((tid % HD) >> 5) & 1)) * 16;
+            const int pair = ((tid % HD) >> 6) * 32 + 8 * (((tid % HD) >> 5) & 1);     // first dim; the others: + 1 .. 7, + 16 .. 23
+            u32x4 lo[ROUNDS], hi[ROUNDS];
+            int seg[ROUNDS];
+            float sc[ROUNDS];
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int i = k * NB + tid / HD, j = (d + i) * 32 + r;
+                lo[k] = hi[k] = u32x4{0, 0, 0, 0};
+                seg[k] = 0;
+                sc[k] = 1.f;
+                if (tid < NB * HD && d + i < end && j < left) {
+                    const int s = source_row(R, j, seg[k]);
+                    const char* q = p + (size_t)(s >> 5) * (32 * HD) + at + ((s & 31) - r) * 16;
+                    lo[k] = *(const u32x4*)q;
+                    hi[k] = *(const u32x4*)(q + HD * 16);
+                    sc[k] = kv8_scale(ex[2 * (s >> 5)]);
+                }
+            }
+            float f[ROUNDS][2][2][8];                  // [unit][half][dim]
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                float mk = 0.f;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    float (&x)[8] = f[k][0][hf], (&y)[8] = f[k][1][hf];
+                    float t[4];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        four_values(lo[k][hf * 2 + q], sc[k], t);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) x[q * 4 + z] = t[z];
+                        four_values(hi[k][hf * 2 + q], sc[k], t);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) y[q * 4 + z] = t[z];
+                    }
+                    if (seg[k] > 0) turn_pairs<ST>(st->table[seg[k] - 1] + pair + 16 * hf, x, y);
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) mk = larger(mk, x[z], y[z]);
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) m[k * NB + b] = tid / HD == b ? mk : 0.f;
+            }
+            exponents_of(m, most[turn], e);
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int i = k * NB + tid / HD;
+                int mine = e[k * NB];
+#pragma unroll
+                for (int b = 1; b < NB; ++b) mine = tid / HD == b ? e[k * NB + b] : mine;
+                const float unit = kv8_scale(mine);
+                u32x4 q[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const float (&x)[8] = f[k][u][z >> 1];
+                        const float t[4] = {x[(z & 1) * 4], x[(z & 1) * 4 + 1], x[(z & 1) * 4 + 2], x[(z & 1) * 4 + 3]};
+                        q[u][z] = four_codes(t, unit);
+                    }
+                if (tid < NB * HD && d + i < end) {    // (rows past the end: zeros, as their block has a new exponent)
+                    *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
+                    *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + HD * 16) = q[1];
+                }
+            }
+        } else if (ST == 2 && one_shift(R, d, min(d + G, end), left)) {
+            // Values of blocks whose rows all have one shift: thread = one dim of one block, whose 32 rows are eight words, every one cut
+            // from two neighbouring words of the source (four rows each; word w of a dim: unit w % 2, word w / 2 of it, in block w / 8).
+            constexpr int NB = 256 / HD < G ? 256 / HD : G, ROUNDS = G / NB;      // (two blocks of 64 dims: half the threads)
+            const int dim = tid % HD, at = ((dim >> 5) * 64 + (dim & 31)) * 16, lastw = (len - 1) >> 2;
+            float f[ROUNDS][8][4];
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int i = __builtin_amdgcn_readfirstlane(min(k * NB + tid / HD, G - 1));     // (whole waves have one block)
                 int seg;
-                const int s0 = source_row(R, d * 32 + r0, seg);
-                int r1 = min(32, left - d * 32);       // rows [r0, r1) lie in one segment: s0 + r - r0
-                if (seg < R.n) r1 = min(r1, r0 + R.first[seg] - s0);
-                for (int sb = s0 >> 5; sb <= (s0 + r1 - r0 - 1) >> 5; ++sb) {
-                    const int off = sb * 32 - s0 + r0;   // row c of the source block is row c + off here
-                    if constexpr (ST == 2) {
-                        const float sc = kv8_scale(ex[2 * sb]);
-                        for (int u = tid; u < HD * 2; u += 256) {
-                            const int lane = u & 63, g = lane >> 5, e = (u >> 6) * 32 + (lane & 31);
-                            const u32x4 q = *(const u32x4*)(p + (size_t)sb * (32 * HD) + u * 16);
+                const int s0 = __builtin_amdgcn_readfirstlane(d + i < end ? source_row(R, (d + i) * 32, seg) : 0);
+                uint32_t word[9];
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                float f[4];
-                                kv8_values(q[x], sc, f);
+                for (int x = 0; x < 9; ++x) {
+                    const int wi = min((s0 >> 2) + x, lastw);
+                    word[x] = *(const uint32_t*)(p + (size_t)(wi >> 3) * (32 * HD) + (wi & 1) * 512 + ((wi & 7) >> 1) * 4 + at);
+                }
+                const int blk = s0 >> 5;
+                const float sa = kv8_scale(__builtin_amdgcn_readfirstlane(ex[2 * blk]));
+                const float sb = kv8_scale(__builtin_amdgcn_readfirstlane(ex[2 * min(blk + 1, (len - 1) >> 5)]));
+                const int live = d + i < end ? left - (d + i) * 32 : 0;      // rows of it that are not past the end
+                float mk = 0.f;
 #pragma unroll
-                                for (int y = 0; y < 4; ++y) {
-                                    const int to = v8_row(x * 4 + y, g) + off;
-                                    if (to >= r0 && to < r1) tile[to][e] = __builtin_bit_cast(uint16_t, (__bf16)f[y]);
+                for (int x = 0; x < 8; ++x) {          // rows 4 x ..
+                    kv8_values(__builtin_amdgcn_alignbyte(word[x + 1], word[x], s0 & 3), 1.f, f[k][x]);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) f[k][x][y] *= (s0 & 31) + 4 * x + y < 32 ? sa : sb;
+                }
+                if (live < 32)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) f[k][x][y] = 4 * x + y < live ? f[k][x][y] : 0.f;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) mk = larger(larger(mk, f[k][x][0], f[k][x][1]), f[k][x][2], f[k][x][3]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) m[k * NB + b] = tid / HD == b ? mk : 0.f;
+            }
+            exponents_of(m, most[turn], e);
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int i = k * NB + tid / HD;
+                int mine = e[k * NB];
+#pragma unroll
+                for (int b = 1; b < NB; ++b) mine = tid / HD == b ? e[k * NB + b] : mine;
+                const float unit = kv8_scale(mine);
+                u32x4 q[2];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) q[x & 1][x >> 1] = four_codes(f[k][x], unit);
+                if (tid < NB * HD && d + i < end) {
+                    *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
+                    *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + 512) = q[1];
+                }
+            }
+        } else if constexpr (TILES) {
+            // the blocks are put together in LDS, segment by segment of rows with one shift
+            __syncthreads();                           // the tiles' last readers are done
+            for (int i = 0; i < G && d + i < end; ++i)
+                for (int r0 = 0; r0 < 32 && (d + i) * 32 + r0 < left;) {
+                    int seg;
+                    const int s0 = source_row(R, (d + i) * 32 + r0, seg);
+                    int r1 = min(32, left - (d + i) * 32);     // rows [r0, r1) lie in one segment: s0 + r - r0
+                    if (seg < R.n) r1 = min(r1, r0 + R.first[seg] - s0);
+                    for (int sb = s0 >> 5; sb <= (s0 + r1 - r0 - 1) >> 5; ++sb) {
+                        const int off = sb * 32 - s0 + r0;       // row c of the source block is row c + off here
+                        if constexpr (ST == 2) {
+                            const float sc = kv8_scale(ex[2 * sb]);
+                            for (int u = tid; u < HD * 2; u += 256) {
+                                const int lane = u & 63, g = lane >> 5, dim = (u >> 6) * 32 + (lane & 31);
+                                const u32x4 q = *(const u32x4*)(p + (size_t)sb * (32 * HD) + u * 16);
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    float f[4];
+                                    kv8_values(q[x], sc, f);
+#pragma unroll
+                                    for (int y = 0; y < 4; ++y) {
+                                        const int to = v8_row(x * 4 + y, g) + off;
+                                        if (to >= r0 && to < r1) tile[i][to][dim] = __builtin_bit_cast(uint16_t, (__bf16)f[y]);
+                                    }
+                                }
+                            }
+                        } else {
+                            for (int u = tid; u < HD * 4; u += 256) {
+                                const int lane = u & 63, g = lane >> 5, pe = u >> 6, dim = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
+                                const u16x8 q = *(const u16x8*)((const uint16_t*)p + (size_t)sb * (32 * HD) + u * 8);
+#pragma unroll
+                                for (int x = 0; x < 8; ++x) {
+                                    const int to = half * 16 + g * 4 + (x >> 2) * 8 + (x & 3) + off;
+                                    if (to >= r0 && to < r1) tile[i][to][dim] = q[x];
                                 }
                             }
                         }
-                    } else {
-                        for (int u = tid; u < HD * 4; u += 256) {
-                            const int lane = u & 63, g = lane >> 5, pe = u >> 6, e = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
-                            const u16x8 q = *(const u16x8*)((const uint16_t*)p + (size_t)sb * (32 * HD) + u * 8);
-#pragma unroll
-                            for (int x = 0; x < 8; ++x) {
-                                const int to = half * 16 + g * 4 + (x >> 2) * 8 + (x & 3) + off;
-                                if (to >= r0 && to < r1) tile[to][e] = q[x];
-                            }
-                        }
                     }
+                    r0 = r1;
                 }
-                r0 = r1;
-            }
             __syncthreads();
-            if constexpr (ST == 2)
-                for (int i = tid; i < min(32, left - d * 32) * (HD / 8); i += 256) {
-                    const u16x8 v = *(const u16x8*)&tile[i / (HD / 8)][(i % (HD / 8)) * 8];
+            if constexpr (ST == 2) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) m = max(m, finite_bits(bf16_bits_to_float(v[x])));
-                }
-        }
-        int e = 0;
-        if constexpr (ST == 2) {
+                for (int i = 0; i < G; ++i)
+                    for (int k = tid; k < min(32, d + i < end ? left - (d + i) * 32 : 0) * (HD / 8); k += 256) {
+                        const u16x8 v = *(const u16x8*)&tile[i][k / (HD / 8)][(k % (HD / 8)) * 8];
 #pragma unroll
-            for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-            if ((tid & 63) == 0) most[turn][tid >> 6] = m;
-        }
-        __syncthreads();                               // every row of this block has been read
-        if constexpr (ST == 2) {
-            e = kv8_exponent(__uint_as_float(max(max(most[turn][0], most[turn][1]), max(most[turn][2], most[turn][3]))));
-            if (tid == 0) ex[2 * d] = (int8_t)e;
-        }
-        const float inv = kv8_scale(-e);
-        if (natural) {
-            // (rows past the end: e4m3 zeros, as their block has a new exponent; the other formats leave them as they are)
-            if (tid < TW && (ST == 2 || j < left)) {
-                store_row8<ST, HD>(p, j, a * 8, nh, inv, lo);
-                store_row8<ST, HD>(p, j, HD / 2 + a * 8, nh, inv, hi);
-            }
-        } else if constexpr (ST == 2) {
-            for (int u = tid; u < HD * 2; u += 256) {
-                const int lane = u & 63, g = lane >> 5, dim = (u >> 6) * 32 + (lane & 31);
-                u32x4 q;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    float f[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int row = v8_row(x * 4 + y, g);
-                        f[y] = d * 32 + row < left ? bf16_bits_to_float(tile[row][dim]) : 0.f;
+                        for (int x = 0; x < 8; x += 2) m[i] = larger(m[i], bf16_bits_to_float(v[x]), bf16_bits_to_float(v[x + 1]));
                     }
-                    q[x] = kv8_four(f, inv);
-                }
-                *(u32x4*)(p + (size_t)d * (32 * HD) + u * 16) = q;
+                exponents_of(m, most[turn], e);
             }
-        } else if constexpr (ST == 1) {
-            for (int u = tid; u < HD * 4; u += 256) {
-                const int lane = u & 63, g = lane >> 5, pe = u >> 6, dim = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
-                u16x8* to = (u16x8*)((uint16_t*)p + (size_t)d * (32 * HD) + u * 8);
-                u16x8 q = *to;
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int row = half * 16 + g * 4 + (x >> 2) * 8 + (x & 3);
-                    if (d * 32 + row < left) q[x] = tile[row][dim];
+            for (int i = 0; i < G; ++i) {
+                if (d + i >= end) break;
+                for (int u = tid; u < HD * (ST == 2 ? 2 : 4); u += 256) {
+                    const int lane = u & 63, g = lane >> 5, pe = u >> 6, dim = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
+                    if constexpr (ST == 2) {
+                        u32x4 q;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            float f[4];
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const int row = v8_row(x * 4 + y, g);
+                                f[y] = (d + i) * 32 + row < left ? bf16_bits_to_float(tile[i][row][dim]) : 0.f;
+                            }
+                            q[x] = four_codes(f, kv8_scale(e[i]));
+                        }
+                        *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + u * 16) = q;
+                    } else {
+                        u16x8* to = (u16x8*)((uint16_t*)p + (size_t)(d + i) * (32 * HD) + u * 8);
+                        u16x8 q = *to;
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            const int row = half * 16 + g * 4 + (x >> 2) * 8 + (x & 3);
+                            if ((d + i) * 32 + row < left) q[x] = tile[i][row][dim];
+                        }
+                        *to = q;
+                    }
                 }
-                *to = q;
             }
         }
+        if constexpr (ST == 2)
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (tid == i && d + i < end) ex[2 * (d + i)] = (int8_t)e[i];
     }
 }
 
@@ -286,18 +502,20 @@ void launch_kv_drop(int storage, const KvPlanes& c, int seq, int nh, int hd, int
     for (int i = 0; i < R.n; ++i) left -= R.count[i] < len_hi - R.first[i] ? R.count[i] : (len_hi > R.first[i] ? len_hi - R.first[i] : 0);
     const int d0 = R.first[0] >> 5, d1 = (left + 31) >> 5, shift = R.count[0] >> 5;
     // Runs of `shift` blocks, all at once in each, where one workgroup per (layer, head, plane) would leave the chip half empty and
-    // the runs are few; else one launch in which every workgroup walks its blocks in order.
+    // the runs are few and long; else one launch in which every workgroup walks its blocks in order.
     const int walkers = layers * nh * 2;
-    const bool runs = shift > 1 && walkers < 2048 && (d1 - d0 + shift - 1) / shift <= 32;
+    const bool runs = shift >= 16 && walkers < 2048 && (d1 - d0 + shift - 1) / shift <= 32;
     for (int d = d0; d < d1; d += runs ? shift : d1 - d0) {
         const int e = runs ? (d + shift < d1 ? d + shift : d1) : d1;
-        const dim3 grid(nh * (runs ? e - d : 1), layers, 2);
-#define DROP(ST_, HD_) hipLaunchKernelGGL((k_kv_drop<ST_, HD_>), grid, dim3(256), 0, s, c, seq, nh, R, st, d, e)
+        const dim3 grid(nh * (runs ? (e - d + 1) / 2 : 1), layers, 2);
+#define DROP_G(ST_, HD_, G_) hipLaunchKernelGGL((k_kv_drop<ST_, HD_, G_>), grid, dim3(256), 0, s, c, seq, nh, R, st, d, e)
+#define DROP(ST_, HD_) do { if (runs || walkers >= 1024) DROP_G(ST_, HD_, 2); else DROP_G(ST_, HD_, 4); } while (0)
 #define DROP2(ST_) do { if (hd == 128) DROP(ST_, 128); else DROP(ST_, 64); } while (0)
         if (storage == 0) DROP2(0);
         else if (storage == 1) DROP2(1);
         else DROP2(2);
 #undef DROP2
 #undef DROP
+#undef DROP_G
     }
 }
