@@ -49,22 +49,24 @@ static __device__ __forceinline__ int kv8_exponent(float most) {
     const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
     return min(max(e, KV8_E_MIN), KV8_E_MAX);
 }
-// two values, already divided by their scale, to two codes (low half of the result). The clamp is for rows that have no say in
-// the exponent any more (past the sequence's end); v_med3 would lose a NaN, hence the selects.
-static __device__ __forceinline__ uint32_t kv8_pair(float a, float b) {
-    const float ca = fminf(fmaxf(a, -448.f), 448.f), cb = fminf(fmaxf(b, -448.f), 448.f);
-    const float nan = __builtin_nanf("");
-    const bool fa = fabsf(a) < __builtin_inff(), fb = fabsf(b) < __builtin_inff();
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fa ? ca : nan, fb ? cb : nan, 0, false) & 0xffffu;
+// Four values to codes of a block whose exponent counts them: none is beyond 448 units, and what is not finite becomes NaN.
+static __device__ __forceinline__ uint32_t kv8_codes(const float (&f)[4], float scale) {
+    typedef __attribute__((ext_vector_type(2))) short s16x2;
+    s16x2 q = {0, 0};
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[0], f[1], scale, false);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[2], f[3], scale, true);
+    return __builtin_bit_cast(uint32_t, q);
 }
-static __device__ __forceinline__ uint32_t kv8_four(const float (&f)[4], float inv) {
-    return kv8_pair(f[0] * inv, f[1] * inv) | (kv8_pair(f[2] * inv, f[3] * inv) << 16);
+// The same of rows that have no say in it (past the sequence's end): held at 448 units.
+static __device__ __forceinline__ float kv8_held(float f, float scale) {
+    const float most = 448.f * scale;
+    return fabsf(f) < __builtin_inff() ? fminf(fmaxf(f, -most), most) : f;
 }
 // four codes to their values
 static __device__ __forceinline__ void kv8_values(uint32_t codes, float scale, float (&f)[4]) {
     typedef __attribute__((ext_vector_type(2))) float f32x2;
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
-    f[0] = lo.x * scale; f[1] = lo.y * scale; f[2] = hi.x * scale; f[3] = hi.y * scale;
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+    f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
 }
 // eight codes to eight bfloat16 values: a matrix operand
 static __device__ __forceinline__ bf16x8 kv8_widen(uint32_t c0, uint32_t c1, float scale) {

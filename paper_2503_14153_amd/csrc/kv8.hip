@@ -37,6 +37,13 @@ static __device__ __forceinline__ void kept_rows(RowTile<HD>& tile, const uint8_
     }
 }
 
+static __device__ __forceinline__ uint32_t largest_of(const u16x8& v) {
+    uint32_t m = v[0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) m = max(m, (uint32_t)v[x]);
+    return m;
+}
+
 // The tile's exponents from its first `valid` rows (those that count), the codes of all 32. Every thread of the workgroup calls it.
 template <int HD>
 static __device__ __forceinline__ void encode_block(const RowTile<HD>& tile, uint8_t* kb, uint8_t* vb, int8_t* ex, int valid) {
@@ -44,13 +51,21 @@ static __device__ __forceinline__ void encode_block(const RowTile<HD>& tile, uin
     __shared__ uint32_t most[2][4];
     const int tid = threadIdx.x;
     __syncthreads();                                   // the tile is whole
-    uint32_t m[2] = {0, 0};                            // largest finite magnitude, as bits: they order like the numbers
+    uint32_t m[2];                                     // largest finite magnitude, as bits: they order like the numbers
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        for (int i = tid; i < valid * PC; i += 256) {
-            const u16x8 v = *(const u16x8*)&tile.t[p][i / PC][(i % PC) * 8];
+        u16x8 v8 = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int i = tid; i < valid * PC; i += 256)
+            v8 = __builtin_elementwise_max(v8, *(const u16x8*)&tile.t[p][i / PC][(i % PC) * 8] & (u16x8)(0x7fff));
+        m[p] = largest_of(v8);
+        if (__any(m[p] >= 0x7f80u)) {                  // infinities or NaN among them (rare): without those
+            u16x8 f8 = {0, 0, 0, 0, 0, 0, 0, 0};
+            for (int i = tid; i < valid * PC; i += 256) {
+                const u16x8 v = *(const u16x8*)&tile.t[p][i / PC][(i % PC) * 8] & (u16x8)(0x7fff);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) { const uint32_t a = v[x] & 0x7fffu; m[p] = max(m[p], a < 0x7f80u ? a : 0u); }
+                for (int x = 0; x < 8; ++x) f8[x] = v[x] < 0x7f80u && v[x] > f8[x] ? v[x] : f8[x];
+            }
+            m[p] = largest_of(f8);
         }
 #pragma unroll
         for (int o = 32; o; o >>= 1) m[p] = max(m[p], (uint32_t)__shfl_xor((int)m[p], o));
@@ -64,7 +79,7 @@ static __device__ __forceinline__ void encode_block(const RowTile<HD>& tile, uin
     if (tid < 2) ex[tid] = (int8_t)e[tid];
     for (int u = tid; u < 2 * U; u += 256) {
         const int p = u / U, w = u - p * U, i = w >> 6, lane = w & 63, g = lane >> 5;
-        const float inv = kv8_scale(-e[p]);
+        const float unit = kv8_scale(e[p]);
         u32x4 q;
         if (p == 0) {
             const u16x8 a = *(const u16x8*)&tile.t[0][lane & 31][i * 32 + 8 * g], b = *(const u16x8*)&tile.t[0][lane & 31][i * 32 + 16 + 8 * g];
@@ -73,7 +88,10 @@ static __device__ __forceinline__ void encode_block(const RowTile<HD>& tile, uin
                 float f[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) f[x] = bf16_bits_to_float(d < 2 ? a[d * 4 + x] : b[(d - 2) * 4 + x]);
-                q[d] = kv8_four(f, inv);
+                if (valid < 32)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) f[x] = (lane & 31) < valid ? f[x] : kv8_held(f[x], unit);
+                q[d] = kv8_codes(f, unit);
             }
         } else {
 #pragma unroll
@@ -81,7 +99,10 @@ static __device__ __forceinline__ void encode_block(const RowTile<HD>& tile, uin
                 float f[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) f[x] = bf16_bits_to_float(tile.t[1][v8_row(d * 4 + x, g)][i * 32 + (lane & 31)]);
-                q[d] = kv8_four(f, inv);
+                if (valid < 32)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) f[x] = v8_row(d * 4 + x, g) < valid ? f[x] : kv8_held(f[x], unit);
+                q[d] = kv8_codes(f, unit);
             }
         }
         *(u32x4*)((p ? vb : kb) + (size_t)w * 16) = q;
@@ -110,7 +131,7 @@ __global__ __launch_bounds__(256) void k_kv8_rows(Kv8 c, uint16_t* __restrict__ 
                                                   int nh, int seq) {
     constexpr int PC = HD / 8;
     __shared__ __attribute__((aligned(16))) RowTile<HD> tile;
-    const int blk = (row0 >> 5) + blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+    const int blk = (row0 >> 5) + blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
     const size_t at = ((size_t)seq * nh + h) * c.cap_blocks + blk;
     uint8_t* kb = c.k + blockIdx.z * c.code_stride + at * (32 * HD);
     uint8_t* vb = c.v + blockIdx.z * c.code_stride + at * (32 * HD);
@@ -139,7 +160,7 @@ __global__ __launch_bounds__(256) void k_kv8_rows(Kv8 c, uint16_t* __restrict__ 
 
 void launch_kv8_rows(const Kv8& c, void* k_rows, void* v_rows, int row0, int nrows, int nh, int hd, int seq, int layers, int to_cache,
                      hipStream_t s) {
-    const dim3 grid((row0 + nrows - 1) / 32 - row0 / 32 + 1, nh, layers);
+    const dim3 grid(nh, (row0 + nrows - 1) / 32 - row0 / 32 + 1, layers);
     const bool vec = ((((uintptr_t)k_rows) | ((uintptr_t)v_rows)) & 15) == 0;
 #define KV8_ROWS(HD_, TO_, VEC_)                                                                                       \
     hipLaunchKernelGGL((k_kv8_rows<HD_, TO_, VEC_>), grid, dim3(256), 0, s, c, (uint16_t*)k_rows, (uint16_t*)v_rows, row0, nrows, nh, seq)

@@ -165,37 +165,6 @@ static __device__ __forceinline__ void turn_pairs(const double2* __restrict__ ta
 }
 // Values that come from codes are finite or NaN, and a maximum of floats takes no NaN: the plain instruction does.
 static __device__ __forceinline__ float larger(float m, float a, float b) { return fmaxf(fmaxf(m, fabsf(a)), fabsf(b)); }
-// and those that had a say in their block's exponent need no clamp (kv8_four)
-static __device__ __forceinline__ uint32_t four_codes(const float (&f)[4], float scale) {
-    typedef __attribute__((ext_vector_type(2))) short s16x2;
-    s16x2 q = {0, 0};
-    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[0], f[1], scale, false);
-    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[2], f[3], scale, true);
-    return __builtin_bit_cast(uint32_t, q);
-}
-static __device__ __forceinline__ void four_values(uint32_t codes, float scale, float (&f)[4]) {
-    typedef __attribute__((ext_vector_type(2))) float f32x2;
-    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
-    f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
-}
-template <int ST, int HD>
-static __device__ __forceinline__ void store_row8(char* p, int row, int e, int nh, float inv, const float (&f)[8]) {
-    if constexpr (ST == 0) {
-        *(float4*)((float*)p + (size_t)row * nh * HD + e) = make_float4(f[0], f[1], f[2], f[3]);
-        *(float4*)((float*)p + (size_t)row * nh * HD + e + 4) = make_float4(f[4], f[5], f[6], f[7]);
-    } else if constexpr (ST == 1) {
-        u16x8 v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(uint16_t, (__bf16)f[i]);
-        *(u16x8*)((uint16_t*)p + kblk_index(row, e, HD)) = v;
-    } else {
-        const float a[4] = {f[0], f[1], f[2], f[3]}, b[4] = {f[4], f[5], f[6], f[7]};
-        u32x2 q;
-        q.x = four_codes(a, inv);
-        q.y = four_codes(b, inv);
-        *(u32x2*)(p + k8_index(row, e, HD)) = q;
-    }
-}
 // The largest of the workgroup's magnitudes for each of G blocks -> exponents. One barrier, which also ends the reads of
 // those blocks. `most` alternates between turns: the one before it may still be read.
 template <int G>
@@ -315,10 +284,10 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
                     float t[4];
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        four_values(lo[k][hf * 2 + q], sc[k], t);
+                        kv8_values(lo[k][hf * 2 + q], sc[k], t);
 #pragma unroll
                         for (int z = 0; z < 4; ++z) x[q * 4 + z] = t[z];
-                        four_values(hi[k][hf * 2 + q], sc[k], t);
+                        kv8_values(hi[k][hf * 2 + q], sc[k], t);
 #pragma unroll
                         for (int z = 0; z < 4; ++z) y[q * 4 + z] = t[z];
                     }
@@ -344,7 +313,7 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
                     for (int z = 0; z < 4; ++z) {
                         const float (&x)[8] = f[k][u][z >> 1];
                         const float t[4] = {x[(z & 1) * 4], x[(z & 1) * 4 + 1], x[(z & 1) * 4 + 2], x[(z & 1) * 4 + 3]};
-                        q[u][z] = four_codes(t, unit);
+                        q[u][z] = kv8_codes(t, unit);
                     }
                 if (tid < NB * HD && d + i < end) {    // (rows past the end: zeros, as their block has a new exponent)
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
@@ -399,7 +368,7 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
                 const float unit = kv8_scale(mine);
                 u32x4 q[2];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) q[x & 1][x >> 1] = four_codes(f[k][x], unit);
+                for (int x = 0; x < 8; ++x) q[x & 1][x >> 1] = kv8_codes(f[k][x], unit);
                 if (tid < NB * HD && d + i < end) {
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + 512) = q[1];
@@ -472,7 +441,7 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
                                 const int row = v8_row(x * 4 + y, g);
                                 f[y] = (d + i) * 32 + row < left ? bf16_bits_to_float(tile[i][row][dim]) : 0.f;
                             }
-                            q[x] = four_codes(f, kv8_scale(e[i]));
+                            q[x] = kv8_codes(f, kv8_scale(e[i]));
                         }
                         *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + u * 16) = q;
                     } else {
