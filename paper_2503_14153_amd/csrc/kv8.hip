@@ -7,6 +7,8 @@
 #include "kv8.h"
 #include "row_ops.h"
 
+#include <algorithm>
+
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
 static __device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
@@ -128,10 +130,10 @@ static __device__ __forceinline__ void piece_to(uint16_t* p, const u16x8& v) {
 }
 template <int HD, bool TO_CACHE, bool VEC>
 __global__ __launch_bounds__(256) void k_kv8_rows(Kv8 c, uint16_t* __restrict__ k_rows, uint16_t* __restrict__ v_rows, int row0, int nrows,
-                                                  int nh, int seq) {
+                                                  int nh, int seq, int b0) {
     constexpr int PC = HD / 8;
     __shared__ __attribute__((aligned(16))) RowTile<HD> tile;
-    const int blk = (row0 >> 5) + blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
+    const int blk = (row0 >> 5) + b0 + blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
     const size_t at = ((size_t)seq * nh + h) * c.cap_blocks + blk;
     uint8_t* kb = c.k + blockIdx.z * c.code_stride + at * (32 * HD);
     uint8_t* vb = c.v + blockIdx.z * c.code_stride + at * (32 * HD);
@@ -160,10 +162,12 @@ __global__ __launch_bounds__(256) void k_kv8_rows(Kv8 c, uint16_t* __restrict__ 
 
 void launch_kv8_rows(const Kv8& c, void* k_rows, void* v_rows, int row0, int nrows, int nh, int hd, int seq, int layers, int to_cache,
                      hipStream_t s) {
-    const dim3 grid(nh, (row0 + nrows - 1) / 32 - row0 / 32 + 1, layers);
+    const int blocks = (row0 + nrows - 1) / 32 - row0 / 32 + 1, step = 32768;      // (a grid's second axis has 65535)
     const bool vec = ((((uintptr_t)k_rows) | ((uintptr_t)v_rows)) & 15) == 0;
 #define KV8_ROWS(HD_, TO_, VEC_)                                                                                       \
-    hipLaunchKernelGGL((k_kv8_rows<HD_, TO_, VEC_>), grid, dim3(256), 0, s, c, (uint16_t*)k_rows, (uint16_t*)v_rows, row0, nrows, nh, seq)
+    for (int b0 = 0; b0 < blocks; b0 += step)                                                                          \
+        hipLaunchKernelGGL((k_kv8_rows<HD_, TO_, VEC_>), dim3(nh, std::min(step, blocks - b0), layers), dim3(256), 0, s, c, \
+                           (uint16_t*)k_rows, (uint16_t*)v_rows, row0, nrows, nh, seq, b0)
 #define KV8_ROWS2(HD_, TO_) do { if (vec) KV8_ROWS(HD_, TO_, true); else KV8_ROWS(HD_, TO_, false); } while (0)
     if (hd == 128) { if (to_cache) KV8_ROWS2(128, true); else KV8_ROWS2(128, false); }
     else           { if (to_cache) KV8_ROWS2(64, true);  else KV8_ROWS2(64, false); }
