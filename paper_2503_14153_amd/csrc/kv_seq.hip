@@ -77,10 +77,34 @@ static __device__ __forceinline__ float odd_float(double d) {
     const uint32_t kept = (lo & 0xe0000000u) | ((cut + 0x1fffffffu) & 0x20000000u);
     return (float)__longlong_as_double((long long)((b & 0xffffffff00000000ull) | kept));
 }
-static __device__ __forceinline__ int source_row(const DropRanges& R, int j, int& segment) {
-    int s = j, i = 0;
-    for (; i < R.n && R.first[i] <= s; ++i) s += R.count[i];
-    segment = i;
+// Where rows come from. Lane i has the first row of what is left that comes from behind range i (none: INT_MAX), and how many rows are
+// gone by then, so a row that is the same for the whole wave takes a ballot, and one per lane a compare for each range.
+struct Gaps { int from, gone; };
+static __device__ __forceinline__ Gaps gaps_of(const DropRanges& R) {
+    const int lane = threadIdx.x & 63;
+    Gaps g = {0x7fffffff, 0};
+    int before = 0;
+    for (int i = 0; i < R.n; ++i) {
+        if (lane == i) g = {R.first[i] - before, before + R.count[i]};
+        before += R.count[i];
+    }
+    return g;
+}
+static __device__ __forceinline__ int segment_at(const Gaps& g, int j) {
+    return (int)__popcll(__ballot(g.from <= __builtin_amdgcn_readfirstlane(j)));
+}
+static __device__ __forceinline__ int gone_before(const Gaps& g, int segment) {
+    return segment ? __builtin_amdgcn_readlane(g.gone, segment - 1) : 0;
+}
+static __device__ __forceinline__ int source_row(const Gaps& g, int n, int j, int& segment) {      // (all lanes of the wave)
+    segment = 0;
+    int s = j;
+    for (int i = 0; i < n; ++i) {
+        const bool behind = __builtin_amdgcn_readlane(g.from, i) <= j;
+        const int gone = __builtin_amdgcn_readlane(g.gone, i);
+        segment += behind ? 1 : 0;
+        s = behind ? j + gone : s;
+    }
     return s;
 }
 
@@ -180,13 +204,10 @@ static __device__ __forceinline__ void exponents_of(float (&m)[G], float (*most)
     for (int i = 0; i < G; ++i) e[i] = kv8_exponent(fmaxf(fmaxf(most[i][0], most[i][1]), fmaxf(most[i][2], most[i][3])));
 }
 
-// Do the rows of every block of [d, end) come from neighbouring rows? (The same answer in every thread.)
-static __device__ __forceinline__ bool one_shift(const DropRanges& R, int d, int end, int left) {
-    for (int b = d; b < end; ++b) {
-        int s;
-        const int j = b * 32, j1 = min(j + 31, left - 1);
-        if (source_row(R, j1, s) - source_row(R, j, s) != j1 - j) return false;
-    }
+// Does every block of [d, end) lie in one segment?
+static __device__ __forceinline__ bool one_shift(const Gaps& g, int d, int end, int left) {
+    for (int b = d; b < end; ++b)
+        if (segment_at(g, b * 32) != segment_at(g, min(b * 32 + 31, left - 1))) return false;
     return true;
 }
 
@@ -204,8 +225,11 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
     const int heads = ST == 0 ? 1 : nh;                // (float32: a row holds all heads)
     char* p = c.p[plane] + blockIdx.y * c.layer + ((size_t)seq * heads + (ST == 0 ? 0 : h)) * c.head + (ST == 0 ? (size_t)h * HD * 4 : 0);
     int8_t* ex = ST == 2 ? (int8_t*)(c.ex + blockIdx.y * c.ex_layer + ((size_t)seq * nh + h) * c.ex_head) + plane : nullptr;
+    const Gaps gaps = gaps_of(R);
     int turn = 0;
-    for (int d = d0 + ((int)blockIdx.x / nh) * G; d < end; d += walkers * G, turn ^= 1) {
+    for (int at_block = d0 + ((int)blockIdx.x / nh) * G; at_block < end; at_block += walkers * G, turn ^= 1) {
+        int d = at_block;
+        asm("" : "+s"(d));                             // (else every row's distance from the end is a register that is counted along)
         float m[G] = {};
         int e[G] = {};
         if (ST != 2 && (plane == 0 || !TILES)) {       // rows as pieces of dims
@@ -215,9 +239,9 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
 #pragma unroll
             for (int i = 0; i < G; ++i) {
                 const int j = (d + i) * 32 + r;
-                seg[i] = -1;
-                if (tid < TW && d + i < end && j < left) {
-                    const int s = source_row(R, j, seg[i]);
+                const int s = source_row(gaps, R.n, j, seg[i]);
+                if (!(tid < TW && d + i < end && j < left)) seg[i] = -1;
+                else {
                     lo[i] = load_row8<ST, HD>(p, s, a * 8, nh);
                     hi[i] = load_row8<ST, HD>(p, s, HD / 2 + a * 8, nh);
                 }
@@ -264,10 +288,10 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
             for (int k = 0; k < ROUNDS; ++k) {
                 const int i = k * NB + tid / HD, j = (d + i) * 32 + r;
                 lo[k] = hi[k] = u32x4{0, 0, 0, 0};
-                seg[k] = 0;
                 sc[k] = 1.f;
-                if (tid < NB * HD && d + i < end && j < left) {
-                    const int s = source_row(R, j, seg[k]);
+                const int s = source_row(gaps, R.n, j, seg[k]);
+                if (!(tid < NB * HD && d + i < end && j < left)) seg[k] = 0;
+                else {
                     const char* q = p + (size_t)(s >> 5) * (32 * HD) + at + ((s & 31) - r) * 16;
                     lo[k] = *(const u32x4*)q;
                     hi[k] = *(const u32x4*)(q + HD * 16);
@@ -320,33 +344,37 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + HD * 16) = q[1];
                 }
             }
-        } else if (ST == 2 && one_shift(R, d, min(d + G, end), left)) {
+        } else if (ST == 2 && one_shift(gaps, d, min(d + G, end), left)) {
             // Values of blocks whose rows all have one shift: thread = one dim of one block, whose 32 rows are eight words, every one cut
             // from two neighbouring words of the source (four rows each; word w of a dim: unit w % 2, word w / 2 of it, in block w / 8).
             constexpr int NB = 256 / HD < G ? 256 / HD : G, ROUNDS = G / NB;      // (two blocks of 64 dims: half the threads)
             const int dim = tid % HD, at = ((dim >> 5) * 64 + (dim & 31)) * 16, lastw = (len - 1) >> 2;
             float f[ROUNDS][8][4];
+            uint32_t word[ROUNDS][9];
+            int s0[ROUNDS], ev[ROUNDS];
 #pragma unroll
             for (int k = 0; k < ROUNDS; ++k) {
                 const int i = __builtin_amdgcn_readfirstlane(min(k * NB + tid / HD, G - 1));     // (whole waves have one block)
-                int seg;
-                const int s0 = __builtin_amdgcn_readfirstlane(d + i < end ? source_row(R, (d + i) * 32, seg) : 0);
-                uint32_t word[9];
+                const int j = min(d + i, end - 1) * 32;
+                s0[k] = j + gone_before(gaps, segment_at(gaps, j));
+                ev[k] = ex[2 * min((s0[k] >> 5) + (tid & 1), (len - 1) >> 5)];      // of the block and the one behind it
 #pragma unroll
                 for (int x = 0; x < 9; ++x) {
-                    const int wi = min((s0 >> 2) + x, lastw);
-                    word[x] = *(const uint32_t*)(p + (size_t)(wi >> 3) * (32 * HD) + (wi & 1) * 512 + ((wi & 7) >> 1) * 4 + at);
+                    const int wi = min((s0[k] >> 2) + x, lastw);
+                    word[k][x] = *(const uint32_t*)(p + (size_t)(wi >> 3) * (32 * HD) + (wi & 1) * 512 + ((wi & 7) >> 1) * 4 + at);
                 }
-                const int blk = s0 >> 5;
-                const float sa = kv8_scale(__builtin_amdgcn_readfirstlane(ex[2 * blk]));
-                const float sb = kv8_scale(__builtin_amdgcn_readfirstlane(ex[2 * min(blk + 1, (len - 1) >> 5)]));
+            }
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int i = __builtin_amdgcn_readfirstlane(min(k * NB + tid / HD, G - 1));
+                const float sa = kv8_scale(__builtin_amdgcn_readlane(ev[k], 0)), sb = kv8_scale(__builtin_amdgcn_readlane(ev[k], 1));
                 const int live = d + i < end ? left - (d + i) * 32 : 0;      // rows of it that are not past the end
                 float mk = 0.f;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {          // rows 4 x ..
-                    kv8_values(__builtin_amdgcn_alignbyte(word[x + 1], word[x], s0 & 3), 1.f, f[k][x]);
+                    kv8_values(__builtin_amdgcn_alignbyte(word[k][x + 1], word[k][x], s0[k] & 3), 1.f, f[k][x]);
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) f[k][x][y] *= (s0 & 31) + 4 * x + y < 32 ? sa : sb;
+                    for (int y = 0; y < 4; ++y) f[k][x][y] *= (s0[k] & 31) + 4 * x + y < 32 ? sa : sb;
                 }
                 if (live < 32)
 #pragma unroll
@@ -379,10 +407,9 @@ __global__ __launch_bounds__(256, G == 2 ? 4 : 2) void k_kv_drop(KvPlanes c, int
             __syncthreads();                           // the tiles' last readers are done
             for (int i = 0; i < G && d + i < end; ++i)
                 for (int r0 = 0; r0 < 32 && (d + i) * 32 + r0 < left;) {
-                    int seg;
-                    const int s0 = source_row(R, (d + i) * 32 + r0, seg);
+                    const int seg = segment_at(gaps, (d + i) * 32 + r0), s0 = (d + i) * 32 + r0 + gone_before(gaps, seg);
                     int r1 = min(32, left - (d + i) * 32);     // rows [r0, r1) lie in one segment: s0 + r - r0
-                    if (seg < R.n) r1 = min(r1, r0 + R.first[seg] - s0);
+                    if (seg < R.n) r1 = min(r1, __builtin_amdgcn_readlane(gaps.from, seg) - (d + i) * 32);
                     for (int sb = s0 >> 5; sb <= (s0 + r1 - r0 - 1) >> 5; ++sb) {
                         const int off = sb * 32 - s0 + r0;       // row c of the source block is row c + off here
                         if constexpr (ST == 2) {
