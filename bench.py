@@ -78,6 +78,8 @@ def parse():
                          "7b-batch8 = eight ragged sequences, the model's own drafts, step time only")
     ap.add_argument("--draft-schedule", default="after_accept", choices=["after_accept", "all_nodes"],
                     help="all_nodes = draft heads on every tree row inside the verifying pass (measured slower here)")
+    ap.add_argument("--kv-rows", default="model", choices=["model", "e4m3"],
+                    help="e4m3 = the cache holds its rows in 8 bits (bf16 shapes; not labels, kv-commit)")
     ap.add_argument("--layers", type=int, default=None, help="cut the depth (debugging only; result is labelled)")
     ap.add_argument("--draft", default="planted", choices=["planted", "random"])
     ap.add_argument("--decoding", default="greedy", choices=["greedy", "sampling"],
@@ -132,7 +134,7 @@ def main():
     model = sd.Model(shape, weights, max_rows=256)       # 256: prompt chunks of 256 rows
     del weights
     torch.cuda.empty_cache()
-    kv = sd.KVCache(model, 1, W.kv_cap)
+    kv = sd.KVCache(model, 1, W.kv_cap, rows=args.kv_rows)
     prompt = wl.zipf_prompt(shape.vocab, prompt_len)
     stop = wl.stop_set(shape.vocab, W.stop_frac)
     stop_words = torch.from_numpy(wl.pack_mask_words(stop).view(np.int32)).cuda()
@@ -307,7 +309,7 @@ def main():
         cpu = cpu_baseline(wl, shape, cpu_keep, T, tree_np, stop, n_cache=prompt_len,
                            typical=dict(typical, u=0.5) if args.decoding == "sampling" else None)
 
-    kv_bytes = (prompt_len + state["e"] / 2) * 2.0 * shape.d_model * 2 * shape.n_layers
+    kv_bytes = (prompt_len + state["e"] / 2) * 2.0 * shape.d_model * (2 if args.kv_rows == "model" else 1) * shape.n_layers
     lm_reads = 2 if args.draft_schedule == "after_accept" else 1 + -(-H * ((T + 31) // 32 * 32) // 128)
     step_bytes = weight_bytes(shape, lm_reads) + kv_bytes
     res = {
@@ -317,7 +319,7 @@ def main():
         "config": {"workload": f"{W.name}: {shape.n_layers}-layer d={shape.d_model} Llama-shaped decoder, "
                                f"{H} draft heads top-{k}, {T}-node tree, batch 1, Zipf prompt {prompt_len}, "
                                f"KV cap {W.kv_cap}, 20% stop ids",
-                   "draft_schedule": args.draft_schedule,
+                   "draft_schedule": args.draft_schedule, "kv_rows": args.kv_rows,
                    "decoding": args.decoding, "typical_acceptance": typical if args.decoding == "sampling" else None,
                    "draft_mode": args.draft if args.decoding == "greedy" else "own heads",
                    "planted_accuracy_by_depth": list(p_depth) if (args.draft == "planted" and args.decoding == "greedy") else None},
@@ -335,7 +337,7 @@ def main():
                      "avg_launch_us": gemm_avg_us,
                      "launches_per_step": g["launches"] / args.profile_steps,
                      "algorithmic_bytes_per_launch": g["bytes"] / max(g["launches"], 1)},
-        "attention": {"kernel": "k_attn_whole (few blocks per workgroup), k_tree_attn", "achieved_GBs": attn_gbs, "frac_hbm": attn_gbs / HBM_PEAK_GBS,
+        "attention": {"kernel": "k_attn8" if args.kv_rows == "e4m3" else "k_attn_whole (few blocks per workgroup), k_tree_attn", "achieved_GBs": attn_gbs, "frac_hbm": attn_gbs / HBM_PEAK_GBS,
                       "avg_launch_us": a["ms"] / max(a["launches"], 1) * 1e3},
         "cpu_baseline": cpu,
     }
@@ -359,7 +361,7 @@ def bench_batch(args, torch, wl, sd, W):
     Tp = (T + 31) // 32 * 32
     model = sd.Model(shape, wl.make_weights(shape, device="cuda"), max_rows=B * Tp)
     torch.cuda.empty_cache()
-    kv = sd.KVCache(model, B, W.kv_cap)
+    kv = sd.KVCache(model, B, W.kv_cap, rows=args.kv_rows)
     rng = np.random.Generator(np.random.Philox(key=wl.SEEDS["kvlen"]))
     lens = [int(x) for x in rng.integers(1024, 4097, size=B)]
     prompt = np.concatenate([wl.zipf_prompt(shape.vocab, n, seed=wl.SEEDS["prompt"] + b) for b, n in enumerate(lens)])
@@ -407,14 +409,14 @@ def bench_batch(args, torch, wl, sd, W):
         "config": {"workload": f"{W.name}: {shape.n_layers}-layer d={shape.d_model} Llama-shaped decoder, {H} draft "
                                f"heads top-{k}, {T}-node trees, batch {B}, Zipf prompts of {lens} tokens, KV cap "
                                f"{W.kv_cap}, 20% stop ids",
-                   "draft_schedule": args.draft_schedule, "decoding": "greedy", "draft_mode": "own heads"},
+                   "draft_schedule": args.draft_schedule, "kv_rows": args.kv_rows, "decoding": "greedy", "draft_mode": "own heads"},
         "prefill_tokens_per_s": sum(lens) / prefill_s, "hip_graphs": args.graph,
         "roofline": {"kernel": "projections (weight-streaming MFMA GEMMs: k_gemm_sk; a few rows k_few, k_gemm_kw, many k_gemm_tile)", "bound": "hbm",
                      "achieved": gemm_gbs, "peak": HBM_PEAK_GBS, "unit": "GB/s", "frac": gemm_gbs / HBM_PEAK_GBS,
                      "traffic": None, "avg_launch_us": g["ms"] / max(g["launches"], 1) * 1e3,
                      "launches_per_step": g["launches"] / args.profile_steps,
                      "algorithmic_bytes_per_launch": g["bytes"] / max(g["launches"], 1)},
-        "attention": {"kernel": "k_attn_whole (few blocks per workgroup), k_tree_attn", "achieved_GBs": a["bytes"] / max(a["ms"], 1e-9) / 1e6,
+        "attention": {"kernel": "k_attn8" if args.kv_rows == "e4m3" else "k_attn_whole (few blocks per workgroup), k_tree_attn", "achieved_GBs": a["bytes"] / max(a["ms"], 1e-9) / 1e6,
                       "avg_launch_us": a["ms"] / max(a["launches"], 1) * 1e3},
         "cpu_baseline": None}))
 
