@@ -103,10 +103,11 @@ void launch_rope_rows(const void* x, void* y, const int32_t* pos, const RopeTabl
     const int align = f32 ? 4 : 8, rd = f.rotary;      // elements of 16 bytes
     const bool vec = ((((uintptr_t)x) | ((uintptr_t)y)) & 15) == 0 && ldx % align == 0 && ldy % align == 0 && hd % 8 == 0 &&
                      rd % (interleaved ? 8 : 16) == 0;
-    // four rows per workgroup where there are rows enough to fill the chip that way; else one, and its heads dealt out
-    const int per = n >= 4 * 512 ? ROPE_ROWS : 1, groups = (n + per - 1) / per;
-    int hg = groups >= 512 ? 1 : 512 / groups, hp = (heads + hg - 1) / hg;
-    if (hp < 4) hp = heads < 4 ? heads : 4;            // (a workgroup makes all angles of its row: 4 heads at least share them)
+    // A workgroup's (row, head) pairs: 32 or so pay for its angles (16384 rows of 8 heads, 128 dims of bfloat16: four rows 12.2 us, one
+    // 14.8; of 64 heads: four 104, one 94), where rows fill the chip that way; else one row, its heads dealt out (64 rows of 64 heads: 3.6
+    // us, 3.9 in a workgroup).
+    const int most = heads >= 32 ? 1 : heads >= 16 ? 2 : ROPE_ROWS, per = n >= 512 * most ? most : 1, groups = (n + per - 1) / per;
+    const int hg = groups >= 512 ? 1 : 512 / groups, hp = (heads + hg - 1) / hg;
     const dim3 grid(groups, (heads + hp - 1) / hp);
 #define ROPE(T_, I_, V_)                                                                                               \
     hipLaunchKernelGGL((k_rope_rows<T_, I_, V_>), grid, dim3(256), 0, s, (const T_*)x, (T_*)y, pos, f, n, heads, hp, hd, ldx, ldy, per)
