@@ -1164,7 +1164,7 @@ struct PassGeom : AttnGeom { AttnSplit split; int whole; Attn8Split eight; };   
 // (k_attn_merge counts the parts of sequences that differ in four bits each)
 static Attn8Split split_of_8(const sd_model* m, int B, int Tp, const int* len) {
     const int TB = Tp / 32;
-    return attn8_split(m->cfg.n_heads * ceil_div(TB, attn8_query_blocks(TB)), attn8_resident(TB), B, TB, len, B > 1 ? 15 : m->max_parts);
+    return attn8_split(m->cfg.n_heads * TB, ATTN8_RESIDENT, B, TB, len, B > 1 ? 15 : m->max_parts);
 }
 // M: the pass's rows (a short prompt has fewer than its padded B * Tp).
 static PassGeom pass_geometry(const sd_model* m, const sd_kv* kv, const int32_t* seq, int B, int M, int Tp, int n_hi) {

@@ -17,7 +17,7 @@ struct Attn8 {
     const uint16_t *q, *k, *v;
     int ld, T;
     uint16_t* out; int ldo;
-    int32_t* arrived;                    // zeros, one per (seq, head, query group): see k_attn8
+    int32_t* arrived;                    // zeros, one per (seq, head, query block): see k_attn8
 };
-// natural rows: also merges the parts into `out`
+// natural rows: the launch merges its parts into `out`
 void launch_attn8(const Attn8& a, hipStream_t s, hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);

@@ -2,9 +2,15 @@
 // share, split over workgroups and waves and joined by (max, sum, O) triples; what differs:
 //   * half the bytes: 16 KiB of bfloat16 per block become 8 KiB of codes, and one instruction per two values widens them to
 //     bfloat16 operands, the block's power-of-two scale included. Widened values are exact, so nothing else is rounded for it;
-//   * queries and probabilities enter as ONE bfloat16 term, not two (attn.hip): their rounding, 2^-9 of a value, is far below
-//     that of the codes they meet, 2^-4. Scores, maxima, sums and outputs stay float32;
-//   * what that saves in registers holds three blocks of keys and values per wave, requested that far ahead.
+//   * queries and probabilities enter as ONE bfloat16 term, not two (attn.hip): their rounding, 2^-8 of a value at most, is far below
+//     that of the codes they meet, 2^-4. Scores, maxima, sums and partial outputs stay float32, natural outputs are rounded once;
+//   * what that saves in registers holds two blocks of keys and values per wave, each requested again as soon as it has been used. A wave
+//     counts its loads in flight (nothing may wait for all of them: see the exponents), and they are under way before the length is known.
+//     Three blocks spill, or share their registers with the accumulators in moves (64 rows over 16873: 47 us, 41 with two); with 64
+//     dims there is room for four, which are not faster (24.8 us, 24.6: eight ragged sequences of 32 rows).
+// Bound by the codes' stream where they are many: 134 MB in 32 us (one row over 16384, 32 heads of 128 dims; the same card streams a
+// plain read in 19), 176 MB in 43 (eight ragged sequences of 32 rows, whose parts are whole blocks of work: the longest part has 51, the
+// mean 40), 140 MB in 40 - 42 (64 rows over 16873). Some 7 us are fixed: launch, first loads, the waves' and the parts' merges.
 // S^T = K Q^T puts query t in lane t % 32; exp(S) in its accumulator registers is the next product's operand (values are stored
 // with their rows in that order).
 #include "attn8.h"
@@ -17,7 +23,7 @@ struct Attn8Args {
     const uint8_t *kc, *vc; const int8_t* ex; int cap_blocks; size_t ex_head;
     const int32_t* kv_len;
     RowRef rr;
-    int nh, Tp, TG, nparts;
+    int nh, Tp, nparts;
     float scale_log2;
     float* opart; float2* mlpart;
     const uint32_t* anc; const bf16x8 *qp, *kt, *vt;
@@ -26,31 +32,30 @@ struct Attn8Args {
     Attn8Split split;
 };
 
-// grid (head, entry of the split x query group): the workgroups of a head share an XCD where heads are a multiple of eight.
-// A workgroup is 4 * QB waves: wave w works on query block w % QB of the group (32 rows) and the quarter w / QB of the part's blocks.
-// NAT: natural rows; else packed ones.
-template <int HD, int QB, bool NAT>
-__global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
+// grid (head, entry of the split x block of 32 query rows): the workgroups of a head share an XCD where heads are a multiple of eight, and
+// the query blocks of a part follow one another, so that all but the first find its rows in the caches. (Two query blocks a workgroup,
+// eight waves, and a launch that merges: 64 rows over 1280 / 16873 17.5 / 39.1 us, here 16.4 / 39.9 - 42; in a step's own launch, 64 rows
+// over some 600, 10.3 us, here 8.9.) Wave w has wave w of the part's blocks. NAT: natural rows; else packed ones.
+template <int HD, bool NAT>
+__global__ __launch_bounds__(256, 2) void k_attn8(Attn8Args a) {
     constexpr int KK = HD / 16, EB = HD / 32, NU = HD / 32;        // contraction steps, output blocks, 16-byte units of a block per lane
     constexpr int BLK = 32 * HD;                                   // bytes of a block
     constexpr int VROW = HD + 8;                                   // LDS row of the tree's values (NAT)
-    constexpr bool JOIN = NAT && QB == 1;                          // this launch also merges the parts
     constexpr int RING = 2;                                        // blocks of K and V that a wave has in flight or in registers
     constexpr int TURNS = 64 / RING * RING;                        // blocks between two loads of exponents
-    __shared__ __attribute__((aligned(16))) float4 lds_o[4 * QB * EB * 4 * 64];      // the waves' O; before that the tree's values
-    __shared__ float lds_ml[4 * QB * 2 * 64];
+    __shared__ __attribute__((aligned(16))) float4 lds_o[4 * EB * 4 * 64];      // the waves' O; before that the tree's values
+    __shared__ float lds_ml[4 * 2 * 64];
     static_assert(32 * VROW * 2 <= EB * 4 * 64 * 16, "a wave's tree values fit its part of the merge area");
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, tl = lane & 31;
     const int h = blockIdx.x, nh = a.nh, Tp = a.Tp, TB = Tp >> 5;
-    const int en = blockIdx.y / a.TG, tg = blockIdx.y - en * a.TG;
+    const int en = blockIdx.y / TB, qb = blockIdx.y - en * TB;      // entry, block of query rows
     const uint32_t entry = a.split.slot[en];
     const int b = entry & 255, part = (entry >> 8) & 255, own = entry >> 16;
     const bool MAP = !NAT && a.rr.map != nullptr;
     const int rows = NAT ? a.T : a.rr.len(b);
-    if (tg * QB * 32 >= rows) return;
-    const int quarter = wave / QB, qb = tg * QB + wave % QB;       // this wave's share of the blocks, and its query block
+    if (qb * 32 >= rows) return;
     const int sq = NAT ? b : a.rr.seq(b);
-    const int jw = __builtin_amdgcn_readfirstlane(part * a.split.each[en] + quarter * a.split.share[en]);    // its first cache block
+    const int jw = __builtin_amdgcn_readfirstlane(part * a.split.each[en] + wave * a.split.share[en]);    // its first cache block
     const size_t head = ((size_t)sq * nh + h) * a.cap_blocks;
     const uint8_t* kcb = a.kc + head * BLK + lane * 16;
     const uint8_t* vcb = a.vc + head * BLK + lane * 16;
@@ -74,13 +79,12 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 qf[KK];                                     // queries: B operands of all contraction steps
     {
-        const int blk = min(qb, TB - 1);
         if constexpr (NAT) {
-            const uint16_t* p = a.q + ((size_t)b * a.T + min(blk * 32 + tl, a.T - 1)) * a.ld + h * HD + g * 8;
+            const uint16_t* p = a.q + ((size_t)b * a.T + min(qb * 32 + tl, a.T - 1)) * a.ld + h * HD + g * 8;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const bf16x8*)(p + kk * 16);
         } else {                                       // (the first of the two terms that the rotary stage leaves)
-            const bf16x8* p = a.qp + (((size_t)b * nh + h) * TB + blk) * (KK * 2 * 64) + lane;
+            const bf16x8* p = a.qp + (((size_t)b * nh + h) * TB + qb) * (KK * 2 * 64) + lane;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) qf[kk] = p[kk * 128];
         }
@@ -98,9 +102,9 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
     n = __builtin_amdgcn_readfirstlane(n);
     asm volatile("" : "+s"(n));
     const int nblk = (n + 31) >> 5;
-    const int ntree = part == own - 1 ? min(tg * QB + QB, (rows + 31) >> 5) : 0;   // tree blocks that the rows can see into
+    const int ntree = part == own - 1 ? qb + 1 : 0;                // tree blocks that the rows can see into: no node before its parent
     const int pend = part == own - 1 ? nblk : min(nblk, (part + 1) * a.split.each[en]);
-    const int je = __builtin_amdgcn_readfirstlane(quarter == 3 ? pend : min(pend, jw + a.split.share[en]));   // this wave's blocks [jw, je)
+    const int je = __builtin_amdgcn_readfirstlane(wave == 3 ? pend : min(pend, jw + a.split.share[en]));   // this wave's blocks [jw, je)
     auto block_of = [&](int j) { return max(min(j, je - 1), 0); };   // (past the wave's last: that block again)
 
     f32x16 O[EB];
@@ -195,8 +199,8 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
         }
     }
 
-    // ---- the tree's blocks, dealt to the quarters one by one: bfloat16 rows, masked by the ancestor sets
-    for (int tblk = quarter; tblk < ntree; tblk += 4) {
+    // ---- the tree's blocks, dealt to the waves one by one: bfloat16 rows, masked by the ancestor sets
+    for (int tblk = wave; tblk < ntree; tblk += 4) {
         bf16x8 kf[KK], vf[2 * EB];
         uint32_t vis = 0;
         if constexpr (NAT) {
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
                     for (int s = 0; s < 8; ++s)
                         vf[p * EB + eb][s] = __builtin_bit_cast(__bf16, tv[(p * 16 + 4 * g + 8 * (s >> 2) + (s & 3)) * VROW + eb * 32 + tl]);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            vis = a.anc[(size_t)min(qb * 32 + tl, Tp - 1) * SD_ANC_WORDS + tblk];
+            vis = a.anc[(size_t)(qb * 32 + tl) * SD_ANC_WORDS + tblk];
         } else {
             const bf16x8* kp = a.kt + ((((size_t)b * nh + h) * TB + tblk) * BLK >> 3) + lane;
             const bf16x8* vp = a.vt + ((((size_t)b * nh + h) * TB + tblk) * BLK >> 3) + lane;
@@ -233,7 +237,7 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
             for (int kk = 0; kk < KK; ++kk) kf[kk] = kp[kk * 64];
 #pragma unroll
             for (int i = 0; i < 2 * EB; ++i) vf[i] = vp[i * 64];
-            vis = a.anc[((size_t)b * Tp + min(qb * 32 + tl, Tp - 1)) * SD_ANC_WORDS + tblk];
+            vis = a.anc[((size_t)b * Tp + (qb * 32 + tl)) * SD_ANC_WORDS + tblk];
         }
         f32x16 S;
         bf16x8 pf[2];
@@ -248,7 +252,7 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
             for (int eb = 0; eb < EB; ++eb) O[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[p * EB + eb], pf[p], O[eb], 0, 0, 0);
     }
 
-    // ---- the four waves of a query block meet in LDS; the output tiles are shared out over all waves
+    // ---- the four waves meet in LDS; the output tiles are shared out over them
     __syncthreads();                                   // (the tree's values of every wave have been read)
 #pragma unroll
     for (int eb = 0; eb < EB; ++eb)
@@ -258,13 +262,13 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
     lds_ml[(wave * 2 + 0) * 64 + lane] = mrun;
     lds_ml[(wave * 2 + 1) * 64 + lane] = lrun;
     __syncthreads();
-    for (int ti = wave; ti < QB * EB; ti += 4 * QB) {
-        const int tb = ti / EB, eb = ti % EB;
+    const int t = qb * 32 + tl, eb = wave;
+    if (eb < EB && t < rows) {                         // (a padding row: nobody reads it)
         float mw[4], lw[4], M = NEG_INF;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            mw[w] = lds_ml[((w * QB + tb) * 2 + 0) * 64 + lane];
-            lw[w] = lds_ml[((w * QB + tb) * 2 + 1) * 64 + lane];
+            mw[w] = lds_ml[w * 2 * 64 + lane];
+            lw[w] = lds_ml[(w * 2 + 1) * 64 + lane];
             M = fmaxf(M, mw[w]);
         }
         const float Muse = (M == NEG_INF) ? 0.f : M;
@@ -274,15 +278,13 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
             sc[w] = exp2f(mw[w] - Muse);               // exp2(-inf) = 0 for a wave that saw nothing
             L += sc[w] * lw[w];
         }
-        const float ltot = L + __shfl_xor(L, 32);
-        const int t = (tg * QB + tb) * 32 + tl;
-        if (t >= rows) continue;                       // a padding row: nobody reads it
+        const float ltot = L + __shfl_xor(L, 32);      // (the other half of the same row)
         const bool done = NAT && own == 1;             // nothing to merge
         const size_t row = (((size_t)b * nh + h) * a.nparts + part) * Tp + t;
         if (eb == 0 && g == 0 && !done) {
             union { float f[2]; uint64_t u; } ml;
             ml.f[0] = M; ml.f[1] = ltot;
-            if constexpr (JOIN) __hip_atomic_store((uint64_t*)&a.mlpart[row], ml.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if constexpr (NAT) __hip_atomic_store((uint64_t*)&a.mlpart[row], ml.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             else a.mlpart[row] = make_float2(M, ltot);
         }
         const float inv = 1.f / ltot;                  // (every row sees at least itself)
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float4 x = lds_o[((w * QB + tb) * EB + eb) * 4 * 64 + i * 64 + lane];
+                const float4 x = lds_o[(w * EB + eb) * 4 * 64 + i * 64 + lane];
                 acc.x += sc[w] * x.x; acc.y += sc[w] * x.y; acc.z += sc[w] * x.z; acc.w += sc[w] * x.w;
             }
             const int e = eb * 32 + 8 * i + 4 * g;
@@ -300,21 +302,21 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
                 o.f[0] = (__bf16)(acc.x * inv); o.f[1] = (__bf16)(acc.y * inv); o.f[2] = (__bf16)(acc.z * inv); o.f[3] = (__bf16)(acc.w * inv);
                 *(uint64_t*)(a.out + ((size_t)b * a.T + t) * a.ldo + h * HD + e) = o.u;
             } else {
-                store_frag16<JOIN>((bf16x8*)(a.opart + row * HD + e), __builtin_bit_cast(bf16x8, acc));
+                store_frag16<NAT>((bf16x8*)(a.opart + row * HD + e), __builtin_bit_cast(bf16x8, acc));
             }
         }
     }
 
-    // ---- natural rows of one query block: whichever part of this (sequence, head) ends last merges them all (always in the order of
-    // their numbers). The parts were stored past this XCD's L2 (row_ops.h: write-through), and have arrived when this workgroup counts
-    // itself; the last one puts the count back to zero for the next launch.
-    if constexpr (JOIN) {
+    // ---- natural rows: whichever part of this (sequence, head, query block) ends last merges them all, always in the order of their
+    // numbers (one row over 16384: 35.6 us with a launch for it, 32.2 here). The parts were stored past this XCD's L2 (row_ops.h:
+    // write-through), and have arrived when this workgroup counts itself; the last one puts the count back to zero for the next launch.
+    if constexpr (NAT) {
         if (own == 1) return;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         int* last = (int*)lds_ml;
         if (tid == 0) {
-            int32_t* count = a.arrived + ((size_t)b * nh + h) * a.TG + tg;
+            int32_t* count = a.arrived + ((size_t)b * nh + h) * TB + qb;
             const int before = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (before == own - 1) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             *last = before == own - 1;
@@ -322,53 +324,35 @@ __global__ __launch_bounds__(256 * QB, 2) void k_attn8(Attn8Args a) {
         __syncthreads();
         if (!*last) return;                            // (workgroup-uniform)
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        const int first = tg * QB * 32, here = min(QB * 32, rows - first);
-        for (int i = tid; i < here * (HD / 8); i += 256 * QB) {
-            const int t = first + i / (HD / 8), e8 = i % (HD / 8);
+        const int first = qb * 32, here = min(32, rows - first);
+        for (int i = tid; i < here * (HD / 8); i += 256) {
+            const int r = first + i / (HD / 8), e8 = i % (HD / 8);
             float o[8];
-            attn_merge_values(a.opart, a.mlpart, nh, HD, Tp, a.nparts, own, b, h, t, e8, o);
-            bf16x8 r;
+            attn_merge_values(a.opart, a.mlpart, nh, HD, Tp, a.nparts, own, b, h, r, e8, o);
+            bf16x8 v;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) r[x] = (__bf16)o[x];
-            *(bf16x8*)(a.out + ((size_t)b * a.T + t) * a.ldo + h * HD + e8 * 8) = r;
+            for (int x = 0; x < 8; ++x) v[x] = (__bf16)o[x];
+            *(bf16x8*)(a.out + ((size_t)b * a.T + r) * a.ldo + h * HD + e8 * 8) = v;
         }
     }
 }
 
-// The parts of natural rows in several query blocks, merged: one thread per (row, head, 8 dims)
-__global__ __launch_bounds__(256) void k_attn8_merge(Attn8Args a, int hd, int e8_shift) {
-    const int idx = blockIdx.x * blockDim.x + threadIdx.x;
-    const int e8 = idx & ((1 << e8_shift) - 1), t = idx >> e8_shift, h = blockIdx.y, b = blockIdx.z, own = a.split.parts[b];
-    if (t >= a.T || own == 1) return;
-    float o[8];
-    attn_merge_values(a.opart, a.mlpart, a.nh, hd, a.Tp, a.nparts, own, b, h, t, e8, o);
-    bf16x8 r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (__bf16)o[i];
-    *(bf16x8*)(a.out + ((size_t)b * a.T + t) * a.ldo + h * hd + e8 * 8) = r;
-}
-
 void launch_attn8(const Attn8& a, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1) {
-    const int TB = a.Tp / 32, QB = attn8_query_blocks(TB), TG = (TB + QB - 1) / QB;
     const bool nat = a.q != nullptr;
     Attn8Args r;
     r.kc = a.c.k; r.vc = a.c.v; r.ex = a.c.ex; r.cap_blocks = a.c.cap_blocks; r.ex_head = kv8_ex_head(a.c.cap_blocks); r.kv_len = a.kv_len; r.rr = a.rr;
-    r.nh = a.nh; r.Tp = a.Tp; r.TG = TG; r.nparts = a.split.max_parts;
+    r.nh = a.nh; r.Tp = a.Tp; r.nparts = a.split.max_parts;
     r.scale_log2 = 1.4426950408889634f / sqrtf((float)a.hd);
     r.opart = a.opart; r.mlpart = a.mlpart; r.qp = a.qp; r.kt = a.kt; r.vt = a.vt; r.anc = a.anc;
     r.q = a.q; r.k = a.k; r.v = a.v; r.ld = a.ld; r.T = a.T; r.out = a.out; r.ldo = a.ldo; r.arrived = a.arrived;
     r.split = a.split;
-    const dim3 grid(a.nh, a.split.n * TG);
-#define ATT8(HD_, QB_, NAT_)                                                                                          \
+    const dim3 grid(a.nh, a.split.n * (a.Tp / 32));
+#define ATT8(HD_, NAT_)                                                                                                \
     do {                                                                                                               \
-        if (ev0 || ev1) hipExtLaunchKernelGGL((k_attn8<HD_, QB_, NAT_>), grid, dim3(256 * QB_), 0, s, ev0, ev1, 0, r);       \
-        else hipLaunchKernelGGL((k_attn8<HD_, QB_, NAT_>), grid, dim3(256 * QB_), 0, s, r);                                  \
+        if (ev0 || ev1) hipExtLaunchKernelGGL((k_attn8<HD_, NAT_>), grid, dim3(256), 0, s, ev0, ev1, 0, r);            \
+        else hipLaunchKernelGGL((k_attn8<HD_, NAT_>), grid, dim3(256), 0, s, r);                                       \
     } while (0)
-#define ATT8_T(HD_, NAT_) do { if (QB == 2) ATT8(HD_, 2, NAT_); else ATT8(HD_, 1, NAT_); } while (0)
-    if (a.hd == 128) { if (nat) ATT8_T(128, true); else ATT8_T(128, false); }
-    else             { if (nat) ATT8_T(64, true);  else ATT8_T(64, false); }
-#undef ATT8_T
+    if (a.hd == 128) { if (nat) ATT8(128, true); else ATT8(128, false); }
+    else             { if (nat) ATT8(64, true);  else ATT8(64, false); }
 #undef ATT8
-    if (nat && QB == 2 && r.nparts > 1)
-        hipLaunchKernelGGL(k_attn8_merge, dim3((a.T * (a.hd / 8) + 255) / 256, a.nh, a.B), dim3(256), 0, s, r, a.hd, a.hd == 128 ? 4 : 3);
 }

@@ -144,14 +144,15 @@ static inline int attn_whole_parts(int n_heads, int B, int Tp, int n_hi) {
 static inline bool attn_whole_pays_prompt(int Tp, int n_hi) { return (n_hi + 31) / 32 + Tp / 32 <= 32; }
 
 // ---- caches in 8 bits (attn8.hip)
-// Parts of every sequence: one entry per (sequence, part), each a workgroup per head and group of query blocks. The host's bounds
-// fix which cache blocks an entry's four waves (or pairs of waves) start at, so that they can be requested before the device's
-// length is known: part p owns blocks [p * each, (p + 1) * each), quarter q of it `share` of them from p * each + q * share on, the
-// last quarter all that are left; and the last part has no end but the length, so that a launch that is replayed for a longer
-// sequence is still whole. The last part also has the tree's blocks, which count as items when the parts are made.
-// groups: heads x query groups, resident: workgroups that the chip holds at once, most: parts of one sequence that the partials
+// Parts of every sequence: one entry per (sequence, part), each a workgroup per head and block of query rows. The host's bounds
+// fix which cache blocks an entry's four waves start at, so that they can be requested before the device's length is known: part p
+// owns blocks [p * each, (p + 1) * each), quarter q of it `share` of them from p * each + q * share on, the last quarter all that
+// are left; and the last part has no end but the length, so that a launch that is replayed for a longer sequence is still whole.
+// The last part also has the tree's blocks, which count as items when the parts are made.
+// groups: heads x query blocks, resident: workgroups that the chip holds at once, most: parts of one sequence that the partials
 // have room for. Two items per wave before another part is opened: every part fetches the queries and adds a term to the merge.
-struct Attn8Split : AttnSplit { int32_t each[ATTN_SPLIT_MAX], share[ATTN_SPLIT_MAX]; uint8_t parts[32]; };     // parts: of sequence b
+// (One or four items: within 0.5 us of it, 517 to 16873 rows.)
+struct Attn8Split : AttnSplit { int32_t each[ATTN_SPLIT_MAX], share[ATTN_SPLIT_MAX]; };
 static inline Attn8Split attn8_split(int groups, int resident, int B, int TB, const int* len, int most) {
     Attn8Split s = {};
     int want = resident / groups, longest = 0;
@@ -171,7 +172,6 @@ static inline Attn8Split attn8_split(int groups, int resident, int B, int TB, co
     for (int b = 0; b < B; ++b) {
         const int n = parts(b, q), each = (blocks(b) + TB + n - 1) / n;
         if (n > s.max_parts) s.max_parts = n;
-        s.parts[b] = (uint8_t)n;
         for (int p = 0; p < n && s.n < ATTN_SPLIT_MAX; ++p) {
             const int left = blocks(b) - p * each, mine = left < 0 ? 0 : p == n - 1 || left < each ? left : each;
             s.each[s.n] = each;
@@ -181,6 +181,6 @@ static inline Attn8Split attn8_split(int groups, int resident, int B, int TB, co
     }
     return s;
 }
-// Query blocks per workgroup, and the workgroups of it that a compute unit holds
-static inline int attn8_query_blocks(int TB) { return TB >= 2 ? 2 : 1; }
-static inline int attn8_resident(int TB) { return attn8_query_blocks(TB) == 2 ? 256 : 512; }
+// Two workgroups a compute unit, for which the kernel's registers have room. (Three or four a unit, the rest of them waiting: eight ragged
+// sequences of 32 rows 49 and 52 us, with two 43.)
+#define ATTN8_RESIDENT 512
