@@ -8,7 +8,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 // ------------------------------------------------------------------------------------------
 // Fork: the source's blocks, which are contiguous per (layer, plane, head), read once and written to every copy as they are. A
-// pure copy: one 16-byte load and n_dst stores per lane, FORK_U of them in flight.
+// pure copy: one 16-byte load and n_dst stores per lane, FORK_U of them in flight. 16384 rows of 4 layers, 32 heads of 128 dims, in 8
+// bits, to one sequence: 537 MB read and as many written in 190 - 205 us, 5.2 - 5.6 TB/s, what a large copy reaches.
 // grid (pieces of a run, heads x 2 planes, layers); the run's length is the device's, the grid the host's bound.
 #define FORK_U 4
 __global__ __launch_bounds__(256) void k_kv_fork(KvPlanes src, KvPlanes dst, SeqList to, int n_dst, const int32_t* __restrict__ kv_len,
@@ -59,16 +60,19 @@ void launch_kv_fork(const KvPlanes& src, const KvPlanes& dst, const SeqList& to,
 // ------------------------------------------------------------------------------------------
 // Drop: row j of what is left was row j + (dropped before it). Keys are rotated for the new position: R(p') = R(p' - p) R(p), one
 // angle per dim pair and segment between two gaps (table[segment - 1][pair], made by k_drop_setup). The rotation is taken in
-// float64 and reaches the storage format in ONE rounding (via float32 rounded to odd), so where a result lies next to a border
-// of the format does not hang on how the products were taken; 4 multiply-adds per pair beside 2 loads and 2 stores do not count.
+// float64 and reaches the storage format in ONE rounding (via float32 rounded to odd where that matters), so where a result lies next
+// to a border of the format does not hang on how the products were taken.
 //
 // Everything in place: dest rows 32 d .. of a block come from rows at or behind them, so a workgroup that walks the blocks of a
 // (layer, head, plane) in order, G at a time, has read every row before it is overwritten (a barrier between the reads of G
-// blocks and their writes). That is one workgroup per (layer, head, plane): enough where a model has some thousand of them.
-// Where it has fewer, `gridDim.x / nh` workgroups share the blocks of [d0, d1), which the host makes no longer than the shortest
-// shift: none of them then writes what another one still has to read, and the launches follow one another.
-// G: a turn is a chain of memory round trips (exponents, rows, the barrier, the stores, some 5 us). Few walkers take four blocks a
-// turn; where workgroups fill the chip two, in as few registers as let several of them hide one another's chains.
+// blocks and their writes). That is one workgroup per (layer, head, plane): enough where a model has a thousand of them.
+// Where it has fewer, the blocks go in runs of [d0, d1), which the host makes no longer than the shortest shift: a run has a
+// workgroup for every turn of G blocks, none of which then writes what another one still has to read, and the runs' launches follow
+// one another.
+//
+// Bound: a run by loads, stores and some 350 vector instructions a wave and block together (the float64 turn is a third of them): 128
+// blocks of 4 layers, 32 heads of 128 dims, 268 MB in 91 us, 51 at the copy rate. A walk by its turns, each a chain of memory round
+// trips and the conversions of one workgroup: 130 of 700 rows of the same, five turns of two blocks each, 28 us.
 // d rounded to odd: cut to 24 bits, the last one set if anything was cut, so that a later rounding to fewer bits sees on which side
 // of a border d lies. (From the bits: below 29 bits of a float64's fraction, a float32's ends.)
 static __device__ __forceinline__ float odd_float(double d) {
@@ -498,6 +502,10 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
 void launch_kv_drop(int storage, const KvPlanes& c, int seq, int nh, int hd, int layers, const DropRanges& R, const double* freq,
                     int32_t* kv_len, int len_hi, DropState* st, hipStream_t s) {
     hipLaunchKernelGGL(k_drop_setup, dim3(R.n), dim3(64), 0, s, R, freq, hd / 2, kv_len, seq, st);
+    // Runs where one workgroup per (layer, head, plane) would leave the chip half empty, and the shift is long enough to pay for a
+    // launch. us, runs / walks; 256 triples of 128 dims: 16384 rows of 8 bits less 4096 281 / 456, less 512 507 / 587, less 300 (nine
+    // blocks a run) 697 / 635; of bfloat16 466 / 1288, 775 / 1483, 1117 / 1759, 700 rows less 130 (four blocks) 53 / 60. 1024 triples
+    // of 64 dims, 8000 rows less 600: 8 bits 508 / 324, bfloat16 766 / 700.
     int left = len_hi;                                 // the host's bound: what is left of the longest it may be
     for (int i = 0; i < R.n; ++i) left -= R.count[i] < len_hi - R.first[i] ? R.count[i] : (len_hi > R.first[i] ? len_hi - R.first[i] : 0);
     const int d0 = R.first[0] >> 5, d1 = (left + 31) >> 5, shift = R.count[0] >> 5;

