@@ -154,6 +154,7 @@ int sd_kv_read_layers(sd_kv* kv, int32_t seq, int32_t row0, int32_t nrows, void*
  * prompt; a prompt run in a cache of its own that joins a running batch). `dst` may be `src` (then src_seq is not among
  * dst_seqs). Both caches belong to one model (SD_ERR_STATE) and store rows alike (SD_ERR_SHAPE); no sequence is named twice.
  * SD_ERR_KV_FULL if the rows might not fit (judged from the length that the host knows). SD_ERR_STATE for a stream under capture.
+ * A source without a draft state gives none, and a step waits until every sequence of its cache has one (SD_ERR_STATE).
  * The tree rows of the last pass stay those of the sequences that the pass held.            */
 int sd_kv_fork(sd_kv* src, int32_t src_seq, sd_kv* dst, const int32_t* dst_seqs, int32_t n_dst, void* stream);
 /* Drop rows from a sequence and close the gaps (a full cache goes on without a part of its context): rows first[i] ..

@@ -167,7 +167,7 @@ struct sd_kv {
     int32_t* state = nullptr;                // device: kv_len, n_old, root_tok, last_row, cand, io scratch
     int32_t *kv_len, *n_old, *root_tok, *last_row, *cand, *i_nacc, *i_tokens, *i_slots;
     std::vector<int32_t> len_hi;             // host upper bound of the committed lengths
-    bool has_draft = false;
+    uint32_t drafted = 0;                    // sequences with a draft state, one bit each
 };
 
 struct sd_tree {
@@ -682,6 +682,9 @@ extern "C" size_t sd_kv8_bytes(const sd_config* cfg, int32_t batch, int32_t cap)
     return (size_t)cfg->n_layers * batch * cfg->n_heads * ((size_t)blocks * 2 * 32 * cfg->head_dim + kv8_ex_head(blocks));
 }
 
+static uint32_t all_sequences(const sd_kv* kv) { return kv->B >= 32 ? 0xffffffffu : (1u << kv->B) - 1u; }
+static_assert(SD_MAX_BATCH <= 32, "one bit a sequence");
+
 static int create_kv(const sd_model* m, int32_t batch, int32_t cap, void* dev_buf, size_t bytes, bool q8, sd_kv** out) {
     const size_t need = q8 ? sd_kv8_bytes(&m->cfg, batch, cap) : sd_kv_bytes(&m->cfg, batch, cap);
     if (batch < 1 || batch > SD_MAX_BATCH) return fail(SD_ERR_SHAPE, "batch must be in 1..%d", SD_MAX_BATCH);
@@ -824,7 +827,7 @@ extern "C" int sd_kv_set_draft(sd_kv* kv, const int32_t* root_tok, const int32_t
     const sd_config& c = kv->m->cfg;
     launch_copy_i32(root_tok, kv->root_tok, kv->B, cand, kv->cand, kv->B * c.n_medusa * c.topk, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
-    kv->has_draft = true;
+    kv->drafted = all_sequences(kv);
     return SD_OK;
 }
 extern "C" int sd_kv_get_draft(sd_kv* kv, int32_t* root_tok, int32_t* cand, void* stream) {
@@ -909,8 +912,11 @@ extern "C" int sd_kv_fork(sd_kv* src, int32_t src_seq, sd_kv* dst, const int32_t
                    c.n_layers, KvCarried{src->kv_len, src->root_tok, src->cand}, KvCarried{dst->kv_len, dst->root_tok, dst->cand},
                    c.n_medusa * c.topk, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
-    for (int i = 0; i < n_dst; ++i) dst->len_hi[to.seq[i]] = src->len_hi[src_seq];
-    dst->has_draft = dst->has_draft || src->has_draft;
+    for (int i = 0; i < n_dst; ++i) {
+        dst->len_hi[to.seq[i]] = src->len_hi[src_seq];
+        const uint32_t bit = 1u << to.seq[i];
+        dst->drafted = (src->drafted >> src_seq & 1) ? dst->drafted | bit : dst->drafted & ~bit;
+    }
     return SD_OK;
 }
 
@@ -1029,15 +1035,15 @@ extern "C" int sd_tree_create(int32_t T, const int32_t* parent, const int32_t* d
     t->Tp = ceil_div(T, 32) * 32;
     t->H = n_medusa;
     t->topk = topk;
-    const size_t words = (size_t)t->Tp * SD_ANC_WORDS;
-    std::vector<int32_t> host(words + (size_t)3 * T, 0);
+    const size_t words = (size_t)t->Tp * SD_ANC_WORDS, bytes = (words + (size_t)3 * T) * 4;
+    int32_t host[SD_MAX_TREE * (SD_ANC_WORDS + 3)] = {};
     for (int j = 0; j < T; ++j)
         for (int i = j; i >= 0; i = parent[i]) host[(size_t)j * SD_ANC_WORDS + (i >> 5)] |= (int32_t)(1u << (i & 31));
-    std::copy(parent, parent + T, host.begin() + words);
-    std::copy(depth, depth + T, host.begin() + words + T);
-    std::copy(rank, rank + T, host.begin() + words + 2 * T);
-    hipError_t e = hipMalloc((void**)&t->dev, host.size() * 4);
-    if (e == hipSuccess) e = hipMemcpy(t->dev, host.data(), host.size() * 4, hipMemcpyHostToDevice);
+    std::copy(parent, parent + T, host + words);
+    std::copy(depth, depth + T, host + words + T);
+    std::copy(rank, rank + T, host + words + 2 * T);
+    hipError_t e = hipMalloc((void**)&t->dev, bytes);
+    if (e == hipSuccess) e = hipMemcpy(t->dev, host, bytes, hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         if (t->dev) hipFree(t->dev);
         delete t;
@@ -1767,7 +1773,7 @@ extern "C" int sd_prefill(sd_model* m, sd_kv* kv, const int32_t* tokens, const i
     }
     HIP_TRY(hipGetLastError());
     if (m->plan_missing) return fail(SD_ERR_STATE, "sd_prefill: a GEMM launch plan was missing");
-    kv->has_draft = true;
+    kv->drafted = all_sequences(kv);
     return SD_OK;
 }
 
@@ -1778,7 +1784,7 @@ static int step_common(sd_model* m, sd_kv* kv, uint64_t tree_uid, const int32_t*
     const sd_config& c = m->cfg;
     const int B = kv->B, H = c.n_medusa;
     if (kv->m != m) return fail(SD_ERR_STATE, "%s: cache belongs to another model", who);
-    if (!kv->has_draft) return fail(SD_ERR_STATE, "%s: no draft state (call sd_prefill or sd_kv_set_draft first)", who);
+    if (kv->drafted != all_sequences(kv)) return fail(SD_ERR_STATE, "%s: no draft state (call sd_prefill or sd_kv_set_draft first)", who);
     if (pow2_blocks(B * Tp) > m->MBmax)
         return fail(SD_ERR_SHAPE, "%s: %d rows exceed the model's max_rows", who, B * Tp);
     int n_hi = 0;

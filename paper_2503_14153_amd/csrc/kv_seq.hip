@@ -3,6 +3,8 @@
 #include "kv_seq.h"
 #include "row_ops.h"
 
+#include <algorithm>
+
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
@@ -508,7 +510,7 @@ void launch_kv_drop(int storage, const KvPlanes& c, int seq, int nh, int hd, int
     // of 64 dims, 8000 rows less 600: 8 bits 508 / 324, bfloat16 766 / 700.
     int left = len_hi;                                 // the host's bound: what is left of the longest it may be
     for (int i = 0; i < R.n; ++i) left -= R.count[i] < len_hi - R.first[i] ? R.count[i] : (len_hi > R.first[i] ? len_hi - R.first[i] : 0);
-    const int d0 = R.first[0] >> 5, d1 = (left + 31) >> 5, shift = R.count[0] >> 5;
+    const int d0 = R.first[0] >> 5, d1 = (left + 31) >> 5, shift = std::min(R.count[0] >> 5, 32768);   // (a grid's limit)
     const int walkers = layers * nh * 2, least = storage == 2 ? 16 : 8;
     const bool runs = shift >= least && walkers < 1024;
     for (int d = d0; d < d1; d += runs ? shift : d1 - d0) {

@@ -5,6 +5,8 @@
 #include "rope.h"
 #include "row_ops.h"
 
+#include <algorithm>
+
 // how a workgroup's rows and heads are cut: enough workgroups to fill the chip, and rows enough to share the angles' set-up
 #define ROPE_ROWS 4
 
@@ -107,12 +109,16 @@ void launch_rope_rows(const void* x, void* y, const int32_t* pos, const RopeTabl
     // A workgroup's (row, head) pairs: 32 or so pay for its angles (16384 rows of 8 heads, 128 dims of bfloat16: four rows 12.2 us, one
     // 14.8; of 64 heads: four 104, one 94), where rows fill the chip that way; else one row, its heads dealt out (64 rows of 64 heads: 3.6
     // us, 3.9 in a workgroup).
-    const int most = heads >= 32 ? 1 : heads >= 16 ? 2 : ROPE_ROWS, per = n >= 512 * most ? most : 1, groups = (n + per - 1) / per;
+    const int most = heads >= 32 ? 1 : heads >= 16 ? 2 : ROPE_ROWS, per = n >= 512 * most ? most : 1, groups = (n - 1) / per + 1;
     const int hg = groups >= 512 ? 1 : 512 / groups, hp = (heads + hg - 1) / hg;
-    const dim3 grid(groups, (heads + hp - 1) / hp);
+    const int step = 1 << 20;                          // rows a launch (a grid's limit)
 #define ROPE(T_, I_, V_)                                                                                               \
-    hipLaunchKernelGGL((k_rope_rows<T_, I_, V_>), grid, dim3(256), 0, s, (const T_*)x, (T_*)y, pos, f, n, heads, hp, hd, ldx, ldy, per)
-#define ROPE2(T_, I_) do { if (vec) ROPE(T_, I_, true); else ROPE(T_, I_, false); } while (0)
+    for (int r = 0; r < n; r += std::min(step, n - r)) {                                                               \
+        const int some = std::min(step, n - r);                                                                        \
+        hipLaunchKernelGGL((k_rope_rows<T_, I_, V_>), dim3((some - 1) / per + 1, (heads + hp - 1) / hp), dim3(256), 0, s, \
+                           (const T_*)x + r * ldx, (T_*)y + r * ldy, pos + r, f, some, heads, hp, hd, ldx, ldy, per);   \
+    }
+#define ROPE2(T_, I_) do { if (vec) { ROPE(T_, I_, true) } else { ROPE(T_, I_, false) } } while (0)
     if (f32) { if (interleaved) ROPE2(float, true); else ROPE2(float, false); }
     else     { if (interleaved) ROPE2(uint16_t, true); else ROPE2(uint16_t, false); }
 #undef ROPE2

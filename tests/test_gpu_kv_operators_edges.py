@@ -271,3 +271,36 @@ def test_offsets_past_32_bits(sd, rows):
             sees = torch.cat([torch.ones(16, left, dtype=torch.bool), ref.ancestors(parent)], dim=1)
             want, spread, reach = ref.attention(args[0][b].cpu(), keys, values, sees)
             assert bool(((out[b].double().cpu() - want).abs() <= ref.attention_bound(want, spread, reach, dim, left + 16)).all())
+
+
+def test_a_step_needs_a_draft_state_of_every_sequence(sd):
+    model = model_of(sd, layers=1, heads=4, dim=64)
+    ready, bare = sd.KVCache(model, 1, 100, rows="e4m3"), sd.KVCache(model, 1, 100, rows="e4m3")
+    sd.prefill(model, ready, torch.arange(20, dtype=torch.int32, device="cuda"), [20])
+    kv = sd.KVCache(model, 2, 100, rows="e4m3")
+
+    def refused():
+        with pytest.raises(sd.SpecDecError) as e:
+            sd.greedy_step(model, kv)
+        assert e.value.name == "SD_ERR_STATE"
+    refused()
+    ready.fork(0, kv, [1])
+    refused()
+    ready.fork(0, kv, [0])
+    a = sd.greedy_step(model, kv)
+    assert kv.len() == [21, 21] and torch.equal(a.tokens[0], a.tokens[1])
+    bare.fork(0, kv, [1])
+    refused()
+    kv.fork(0, kv, [1])
+    sd.greedy_step(model, kv)
+    assert kv.len() == [22, 22]
+
+
+def test_more_than_a_million_rows_are_rotated(sd):
+    n = 2 ** 20 + 77
+    x = torch.randn((n, 1, 64), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(torch.bfloat16)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") % 5000
+    rope = sd.Rope(1e4, 64)
+    got = sd.rope_rows(x, pos, rope)
+    for at in (0, 2 ** 20 - 50, 2 ** 20 - 1, n - 60):   # the same rows in calls of their own, to the bit
+        assert torch.equal(got[at:at + 60], sd.rope_rows(x[at:at + 60].contiguous(), pos[at:at + 60].contiguous(), rope))
