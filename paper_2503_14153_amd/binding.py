@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import cached_property
 
 import torch
 
@@ -169,6 +170,10 @@ class Rope:
     magnitude: float = 1.0
 
     def _c(self) -> _Rope:
+        return self._struct
+
+    @cached_property
+    def _struct(self) -> _Rope:
         return _Rope(self.theta, self.rotary_dim, {"half": 0, "interleaved": 1}[self.layout],
                      {"none": 0, "linear": 1, "by_parts": 2}[self.scaling], self.factor, self.low, self.high, self.trained_len,
                      self.magnitude)
@@ -485,11 +490,10 @@ def rope_rows(x: torch.Tensor, pos: torch.Tensor, rope: Rope, *, inverse: bool =
     if out is None:
         out = x.new_empty((n, nh, hd))
     assert out.is_cuda and out.shape == x.shape and out.dtype == x.dtype
-    for t in (x, out):
-        assert n == 0 or (t.stride(2) == 1 and (nh == 1 or t.stride(1) == hd))
-    ld = [t.stride(0) if n > 1 else nh * hd for t in (x, out)]
-    _check(lib().sd_rope_rows(C.byref(rope._c()), 1 if x.dtype == torch.bfloat16 else 0, x.data_ptr(), ld[0], out.data_ptr(), ld[1],
-                              pos.data_ptr(), n, nh, hd, 1 if inverse else 0, _stream()))
+    sx, sy, row = x.stride(), out.stride(), nh * hd
+    assert n == 0 or (sx[2] == sy[2] == 1 and (nh == 1 or sx[1] == sy[1] == hd))
+    _check(lib().sd_rope_rows(C.byref(rope._c()), 1 if x.dtype == torch.bfloat16 else 0, x.data_ptr(), sx[0] if n > 1 else row,
+                              out.data_ptr(), sy[0] if n > 1 else row, pos.data_ptr(), n, nh, hd, 1 if inverse else 0, _stream()))
     return out
 
 
