@@ -458,9 +458,13 @@ def kv_commit_rows(model: Model, kv: KVCache, src_slots: torch.Tensor, n_rows: t
 def _row_distance(t: torch.Tensor) -> int:
     """Elements between the rows of [batch, T, heads, dim] whose heads are contiguous and whose rows lie evenly."""
     B, T, nh, hd = t.shape
-    assert t.is_cuda and t.stride(3) == 1 and (nh == 1 or t.stride(2) == hd)
-    ld = t.stride(1) if T > 1 else t.stride(0) if B > 1 else nh * hd
-    assert B == 1 or t.stride(0) == T * ld
+    assert t.is_cuda
+    if t.is_contiguous():
+        return nh * hd
+    sb, st, sh, se = t.stride()
+    assert se == 1 and (nh == 1 or sh == hd)
+    ld = st if T > 1 else sb if B > 1 else nh * hd
+    assert B == 1 or sb == T * ld
     return ld
 
 
