@@ -304,3 +304,53 @@ def test_more_than_a_million_rows_are_rotated(sd):
     got = sd.rope_rows(x, pos, rope)
     for at in (0, 2 ** 20 - 50, 2 ** 20 - 1, n - 60):   # the same rows in calls of their own, to the bit
         assert torch.equal(got[at:at + 60], sd.rope_rows(x[at:at + 60].contiguous(), pos[at:at + 60].contiguous(), rope))
+
+
+@pytest.mark.parametrize("dtype,rows", FORMATS)
+@pytest.mark.parametrize("ranges", [[(40, 30)], [(10, 600)]])
+def test_nan_stays_in_its_pair(sd, dtype, rows, ranges):
+    heads, dim, n = 4, 64, 700
+    model = model_of(sd, heads=heads, dim=dim, dtype=dtype)
+    kv = sd.KVCache(model, 1, 720, rows=rows)
+    x = layers_of(1, n, heads, dim, 13, dtype)
+    for t in x:
+        for row, head, e in ((5, 0, 3), (39, 1, 40), (50, 2, 0), (71, 3, 63), (650, 0, 31), (699, 2, 32)):
+            t[0, row, head, e] = float("nan")
+    kv.write_layers(0, 0, *(t.cuda() for t in x))
+    kv.set_len([n])
+    kv.fork(0, kv2 := sd.KVCache(model, 1, 720, rows=rows), [0])
+    for t, got in zip(x, kv2.read_layers(0, 0, n)):
+        same(got, held(t, rows))
+    kv.drop_rows(0, ranges)
+    left = n - ranges[0][1]
+    for p, got in enumerate(kv.read_layers(0, 0, left)):
+        want = after_drop(held(x[p], rows)[0], n, ranges, 1e4, p, dtype, rows)
+        got = got[0].double().cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and int(torch.isnan(want).sum()) >= 3
+        off = (got - want).abs().nan_to_num()
+        assert bool((off <= (2.0 ** -23 * want.abs().nan_to_num() + 1e-14 if dtype == "f32" and p == 0 else 0.0)).all()), float(off.max())
+
+
+def test_attention_over_nan_and_infinite_rows(sd):
+    """A cached NaN is seen by every row of its head and by no other head; one in the tree by its descendants alone."""
+    nh, hd, T, n = 4, 64, 40, 100
+    model = model_of(sd, heads=nh, dim=hd, n_medusa=4, topk=10)
+    tree, parent = tree_of(sd, T, 4, 10)
+    kv, cached = filled(sd, model, [n], 200, 21)
+    q, k, v = qkv(1, T, nh, hd, 22)
+    clean = sd.tree_attention(model, kv, tree, 0, q, k, v)
+    bad_k, bad_v = cached[0][0].clone(), cached[0][1].clone()
+    bad_k[37, 1, 5] = float("inf")
+    bad_v[99, 2, 7] = float("nan")
+    kv.write_rows(0, 0, 0, bad_k.cuda(), bad_v.cuda())
+    out = sd.tree_attention(model, kv, tree, 0, q, k, v)
+    assert torch.equal(out[:, :, [0, 3]], clean[:, :, [0, 3]])
+    assert bool(torch.isnan(out[:, :, 1]).all())
+    assert bool(torch.isnan(out[:, :, 2, 7]).all()) and torch.equal(out[:, :, 2, :7], clean[:, :, 2, :7])
+    kv.write_rows(0, 0, 0, cached[0][0].cuda(), cached[0][1].cuda())
+    k2 = k.clone()
+    k2[0, 3, 0, 0] = float("nan")
+    out = sd.tree_attention(model, kv, tree, 0, q, k2, v)
+    sees = ref.ancestors(parent)[:, 3].cuda()
+    assert torch.equal(torch.isnan(out[0, :, 0]).all(dim=1), sees) and torch.equal(out[0, ~sees], clean[0, ~sees])
+    assert torch.equal(out[:, :, 1:], clean[:, :, 1:])
