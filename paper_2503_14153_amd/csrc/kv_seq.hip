@@ -73,8 +73,9 @@ void launch_kv_fork(const KvPlanes& src, const KvPlanes& dst, const SeqList& to,
 // one another.
 //
 // Bound: a run by loads, stores and some 350 vector instructions a wave and block together (the float64 turn is a third of them): 128
-// blocks of 4 layers, 32 heads of 128 dims, 268 MB in 91 us, 51 at the copy rate. A walk by its turns, each a chain of memory round
-// trips and the conversions of one workgroup: 130 of 700 rows of the same, five turns of two blocks each, 28 us.
+// blocks of 4 layers, 32 heads of 128 dims, 268 MB in 85 - 92 us, 51 at the copy rate. A walk by its turns, each a chain of memory round
+// trips and the conversions of one workgroup, some 4 us: 130 of 700 rows of the same, 18 blocks, four at a time, 27 us. A walk's V blocks
+// of several shifts go by themselves, through LDS: that is 8 us for eight blocks.
 // d rounded to odd: cut to 24 bits, the last one set if anything was cut, so that a later rounding to fewer bits sees on which side
 // of a border d lies. (From the bits: below 29 bits of a float64's fraction, a float32's ends.)
 static __device__ __forceinline__ float odd_float(double d) {
@@ -197,8 +198,8 @@ static __device__ __forceinline__ void turn_pairs(const double2* __restrict__ ta
 static __device__ __forceinline__ float larger(float m, float a, float b) { return fmaxf(fmaxf(m, fabsf(a)), fabsf(b)); }
 // The largest of the workgroup's magnitudes for each of G blocks -> exponents. One barrier, which also ends the reads of
 // those blocks. `most` alternates between turns: the one before it may still be read.
-template <int G>
-static __device__ __forceinline__ void exponents_of(float (&m)[G], float (*most)[4], int (&e)[G]) {
+template <int G, int W>
+static __device__ __forceinline__ void exponents_of(float (&m)[G], float (*most)[W], int (&e)[G]) {
 #pragma unroll
     for (int i = 0; i < G; ++i) {
 #pragma unroll
@@ -207,26 +208,29 @@ static __device__ __forceinline__ void exponents_of(float (&m)[G], float (*most)
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < G; ++i) e[i] = kv8_exponent(fmaxf(fmaxf(most[i][0], most[i][1]), fmaxf(most[i][2], most[i][3])));
+    for (int i = 0; i < G; ++i) {
+        float x = most[i][0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) x = fmaxf(x, most[i][w]);
+        e[i] = kv8_exponent(x);
+    }
 }
 
-// Does every block of [d, end) lie in one segment?
-static __device__ __forceinline__ bool one_shift(const Gaps& g, int d, int end, int left) {
-    for (int b = d; b < end; ++b)
-        if (segment_at(g, b * 32) != segment_at(g, min(b * 32 + 31, left - 1))) return false;
-    return true;
+// Does block b lie in one segment?
+static __device__ __forceinline__ bool one_shift(const Gaps& g, int b, int left) {
+    return segment_at(g, b * 32) == segment_at(g, min(b * 32 + 31, left - 1));
 }
 
-// Blocks a turn. Codes: as many as give every thread two units. The others: two, for registers (16384 rows of bfloat16 less 4096: 468 us
+// Blocks a turn. Codes: as many as give every thread two units (one dim's rows). The others: two, for registers (16384 rows of bfloat16 less 4096: 468 us
 // with two, 542 with four).
-static constexpr int drop_blocks(int storage, int HD) { return storage == 2 ? 256 / HD : 2; }
+static constexpr int drop_blocks(int storage, int HD, int threads) { return storage == 2 ? threads / HD : 2; }
 
-template <int ST, int HD, int G>
-__global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh, DropRanges R, const DropState* __restrict__ st, int d0, int d1) {
+template <int ST, int HD, int G, int TH>
+__global__ __launch_bounds__(TH, 4) void k_kv_drop(KvPlanes c, int seq, int nh, DropRanges R, const DropState* __restrict__ st, int d0, int d1) {
     constexpr int A = HD / 16;                         // pieces of 8 dims + their rotary partners per row
     constexpr int TW = 32 * A;                         // threads that have one
     constexpr bool TILES = ST != 0;                    // values are stored turned: several rows of one dim to a piece
-    __shared__ float most[2][G][4];
+    __shared__ float most[2][G][TH / 64];
     __shared__ __attribute__((aligned(16))) uint16_t tile[TILES ? G : 1][32][HD + 8];
     const int h = blockIdx.x % nh, walkers = gridDim.x / nh, plane = blockIdx.z, tid = threadIdx.x;
     const int len = st->old_len, left = st->new_len;
@@ -236,10 +240,20 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
     char* p = c.p[plane] + blockIdx.y * c.layer + ((size_t)seq * heads + (ST == 0 ? 0 : h)) * c.head + (ST == 0 ? (size_t)h * HD * 4 : 0);
     int8_t* ex = ST == 2 ? (int8_t*)(c.ex + blockIdx.y * c.ex_layer + ((size_t)seq * nh + h) * c.ex_head) + plane : nullptr;
     const Gaps gaps = gaps_of(R);
-    int turn = 0;
-    for (int at_block = d0 + ((int)blockIdx.x / nh) * G; at_block < end; at_block += walkers * G, turn ^= 1) {
-        int d = at_block;
+    int turn = 0, d = d0 + ((int)blockIdx.x / nh) * G, last = min(d + G, end);
+    for (int stop; d < end; turn ^= 1, d = stop) {     // blocks [d, stop) of this workgroup's [.., last)
+        if (d == last) {
+            d += (walkers - 1) * G;
+            last = min(d + G, end);
+            if (d >= end) break;
+        }
         asm("" : "+s"(d));                             // (else every row's distance from the end is a register that is counted along)
+        stop = last;
+        if (ST == 2 && plane == 1) {                   // blocks of one shift each, or one of several
+            stop = d + 1;
+            if (one_shift(gaps, d, left))
+                while (stop < last && one_shift(gaps, stop, left)) ++stop;
+        }
         float m[G] = {};
         int e[G] = {};
         if (ST != 2 && (plane == 0 || !TILES)) {       // rows as pieces of dims
@@ -250,7 +264,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
             for (int i = 0; i < G; ++i) {
                 const int j = (d + i) * 32 + r;
                 const int s = source_row(gaps, R.n, j, seg[i]);
-                if (!(tid < TW && d + i < end && j < left)) seg[i] = -1;
+                if (!(tid < TW && d + i < stop && j < left)) seg[i] = -1;
                 else {
                     lo[i] = load_row8<ST, HD>(p, s, a * 8, nh);
                     hi[i] = load_row8<ST, HD>(p, s, HD / 2 + a * 8, nh);
@@ -278,7 +292,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
 #pragma unroll
             for (int i = 0; i < G; ++i) {
                 const int j = (d + i) * 32 + r;
-                if (tid < TW && d + i < end && j < left) {
+                if (tid < TW && d + i < stop && j < left) {
                     const float x[8] = {f[i][0], f[i][1], f[i][2], f[i][3], f[i][4], f[i][5], f[i][6], f[i][7]};
                     const float y[8] = {f[i][8], f[i][9], f[i][10], f[i][11], f[i][12], f[i][13], f[i][14], f[i][15]};
                     store_row8<ST, HD>(p, j, a * 8, nh, x);
@@ -288,7 +302,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
         } else if (ST == 2 && plane == 0) {
             // Keys: thread = one row of one block and two 16-byte units of it, sixteen dims and their rotary partners: a wave reads and
             // writes whole runs of 512 bytes. (With eight dims to a thread, half units, the launch wrote 2.5 times its bytes.)
-            constexpr int NB = 256 / HD < G ? 256 / HD : G, ROUNDS = G / NB;
+            constexpr int NB = TH / HD < G ? TH / HD : G, ROUNDS = G / NB;
             const int r = tid & 31, at = (((tid % HD) >> 6) * 64 + r + 32 * (((tid % HD) >> 5) & 1)) * 16;
             const int pair = ((tid % HD) >> 6) * 32 + 8 * (((tid % HD) >> 5) & 1);     // first dim; the others: + 1 .. 7, + 16 .. 23
             u32x4 lo[ROUNDS], hi[ROUNDS];
@@ -300,7 +314,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
                 lo[k] = hi[k] = u32x4{0, 0, 0, 0};
                 sc[k] = 1.f;
                 const int s = source_row(gaps, R.n, j, seg[k]);
-                if (!(tid < NB * HD && d + i < end && j < left)) seg[k] = 0;
+                if (!(tid < NB * HD && d + i < stop && j < left)) seg[k] = 0;
                 else {
                     const char* q = p + (size_t)(s >> 5) * (32 * HD) + at + ((s & 31) - r) * 16;
                     lo[k] = *(const u32x4*)q;
@@ -349,15 +363,15 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
                         const float t[4] = {x[(z & 1) * 4], x[(z & 1) * 4 + 1], x[(z & 1) * 4 + 2], x[(z & 1) * 4 + 3]};
                         q[u][z] = kv8_codes(t, unit);
                     }
-                if (tid < NB * HD && d + i < end) {    // (rows past the end: zeros, as their block has a new exponent)
+                if (tid < NB * HD && d + i < stop) {    // (rows past the end: zeros, as their block has a new exponent)
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + HD * 16) = q[1];
                 }
             }
-        } else if (ST == 2 && one_shift(gaps, d, min(d + G, end), left)) {
+        } else if (ST == 2 && one_shift(gaps, d, left)) {
             // Values of blocks whose rows all have one shift: thread = one dim of one block, whose 32 rows are eight words, every one cut
             // from two neighbouring words of the source (four rows each; word w of a dim: unit w % 2, word w / 2 of it, in block w / 8).
-            constexpr int NB = 256 / HD < G ? 256 / HD : G, ROUNDS = G / NB;      // (two blocks of 64 dims: half the threads)
+            constexpr int NB = TH / HD < G ? TH / HD : G, ROUNDS = G / NB;      // (two blocks of 64 dims: half the threads)
             const int dim = tid % HD, at = ((dim >> 5) * 64 + (dim & 31)) * 16, lastw = (len - 1) >> 2;
             float f[ROUNDS][8][4];
             uint32_t word[ROUNDS][9];
@@ -365,7 +379,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
 #pragma unroll
             for (int k = 0; k < ROUNDS; ++k) {
                 const int i = __builtin_amdgcn_readfirstlane(min(k * NB + tid / HD, G - 1));     // (whole waves have one block)
-                const int j = min(d + i, end - 1) * 32;
+                const int j = min(d + i, stop - 1) * 32;
                 s0[k] = j + gone_before(gaps, segment_at(gaps, j));
                 ev[k] = ex[2 * min((s0[k] >> 5) + (tid & 1), (len - 1) >> 5)];      // of the block and the one behind it
 #pragma unroll
@@ -378,7 +392,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
             for (int k = 0; k < ROUNDS; ++k) {
                 const int i = __builtin_amdgcn_readfirstlane(min(k * NB + tid / HD, G - 1));
                 const float sa = kv8_scale(__builtin_amdgcn_readlane(ev[k], 0)), sb = kv8_scale(__builtin_amdgcn_readlane(ev[k], 1));
-                const int live = d + i < end ? left - (d + i) * 32 : 0;      // rows of it that are not past the end
+                const int live = d + i < stop ? left - (d + i) * 32 : 0;      // rows of it that are not past the end
                 float mk = 0.f;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {          // rows 4 x ..
@@ -407,7 +421,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
                 u32x4 q[2];
 #pragma unroll
                 for (int x = 0; x < 8; ++x) q[x & 1][x >> 1] = kv8_codes(f[k][x], unit);
-                if (tid < NB * HD && d + i < end) {
+                if (tid < NB * HD && d + i < stop) {
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at) = q[0];
                     *(u32x4*)(p + (size_t)(d + i) * (32 * HD) + at + 512) = q[1];
                 }
@@ -415,7 +429,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
         } else if constexpr (TILES) {
             // the blocks are put together in LDS, segment by segment of rows with one shift
             __syncthreads();                           // the tiles' last readers are done
-            for (int i = 0; i < G && d + i < end; ++i)
+            for (int i = 0; i < G && d + i < stop; ++i)
                 for (int r0 = 0; r0 < 32 && (d + i) * 32 + r0 < left;) {
                     const int seg = segment_at(gaps, (d + i) * 32 + r0), s0 = (d + i) * 32 + r0 + gone_before(gaps, seg);
                     int r1 = min(32, left - (d + i) * 32);     // rows [r0, r1) lie in one segment: s0 + r - r0
@@ -424,7 +438,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
                         const int off = sb * 32 - s0 + r0;       // row c of the source block is row c + off here
                         if constexpr (ST == 2) {
                             const float sc = kv8_scale(ex[2 * sb]);
-                            for (int u = tid; u < HD * 2; u += 256) {
+                            for (int u = tid; u < HD * 2; u += TH) {
                                 const int lane = u & 63, g = lane >> 5, dim = (u >> 6) * 32 + (lane & 31);
                                 const u32x4 q = *(const u32x4*)(p + (size_t)sb * (32 * HD) + u * 16);
 #pragma unroll
@@ -439,7 +453,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
                                 }
                             }
                         } else {
-                            for (int u = tid; u < HD * 4; u += 256) {
+                            for (int u = tid; u < HD * 4; u += TH) {
                                 const int lane = u & 63, g = lane >> 5, pe = u >> 6, dim = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
                                 const u16x8 q = *(const u16x8*)((const uint16_t*)p + (size_t)sb * (32 * HD) + u * 8);
 #pragma unroll
@@ -456,7 +470,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
             if constexpr (ST == 2) {
 #pragma unroll
                 for (int i = 0; i < G; ++i)
-                    for (int k = tid; k < min(32, d + i < end ? left - (d + i) * 32 : 0) * (HD / 8); k += 256) {
+                    for (int k = tid; k < min(32, d + i < stop ? left - (d + i) * 32 : 0) * (HD / 8); k += TH) {
                         const u16x8 v = *(const u16x8*)&tile[i][k / (HD / 8)][(k % (HD / 8)) * 8];
 #pragma unroll
                         for (int x = 0; x < 8; x += 2) m[i] = larger(m[i], bf16_bits_to_float(v[x]), bf16_bits_to_float(v[x + 1]));
@@ -465,8 +479,8 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
             }
 #pragma unroll
             for (int i = 0; i < G; ++i) {
-                if (d + i >= end) break;
-                for (int u = tid; u < HD * (ST == 2 ? 2 : 4); u += 256) {
+                if (d + i >= stop) break;
+                for (int u = tid; u < HD * (ST == 2 ? 2 : 4); u += TH) {
                     const int lane = u & 63, g = lane >> 5, pe = u >> 6, dim = (pe % (HD / 32)) * 32 + (lane & 31), half = pe / (HD / 32);
                     if constexpr (ST == 2) {
                         u32x4 q;
@@ -497,7 +511,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_drop(KvPlanes c, int seq, int nh,
         if constexpr (ST == 2)
 #pragma unroll
             for (int i = 0; i < G; ++i)
-                if (tid == i && d + i < end) ex[2 * (d + i)] = (int8_t)e[i];
+                if (tid == i && d + i < stop) ex[2 * (d + i)] = (int8_t)e[i];
     }
 }
 
@@ -505,27 +519,31 @@ void launch_kv_drop(int storage, const KvPlanes& c, int seq, int nh, int hd, int
                     int32_t* kv_len, int len_hi, DropState* st, hipStream_t s) {
     hipLaunchKernelGGL(k_drop_setup, dim3(R.n), dim3(64), 0, s, R, freq, hd / 2, kv_len, seq, st);
     // Runs where one workgroup per (layer, head, plane) would leave the chip half empty, and the shift is long enough to pay for a
-    // launch. us, runs / walks; 256 triples of 128 dims: 16384 rows of 8 bits less 4096 281 / 456, less 512 507 / 587, less 300 (nine
-    // blocks a run) 697 / 635; of bfloat16 466 / 1288, 775 / 1483, 1117 / 1759, 700 rows less 130 (four blocks) 53 / 60. 1024 triples
-    // of 64 dims, 8000 rows less 600: 8 bits 508 / 324, bfloat16 766 / 700.
+    // launch. us, runs / walks; 256 triples of 128 dims: 16384 rows of 8 bits less 4096 283 / 456, less 512 (16 blocks a run) 512 / 501, less
+    // 300 697 / 497; of bfloat16 less 4096 466 / 1288, less 512 775 / 1483, less 300 1117 / 1759, 700 rows less 130 (four blocks) 53 / 60.
+    // 1024 triples of 64 dims, 8000 rows less 600: 8 bits 508 / 324, bfloat16 766 / 700.
+    // A walk of codes where walkers are few takes 512 threads: less 300 of 16384 rows 497, with 256 648; 130 of 700 31.4 / 32.2, with 1024
+    // 38.9.
     int left = len_hi;                                 // the host's bound: what is left of the longest it may be
     for (int i = 0; i < R.n; ++i) left -= R.count[i] < len_hi - R.first[i] ? R.count[i] : (len_hi > R.first[i] ? len_hi - R.first[i] : 0);
     const int d0 = R.first[0] >> 5, d1 = (left + 31) >> 5, shift = std::min(R.count[0] >> 5, 32768);   // (a grid's limit)
-    const int walkers = layers * nh * 2, least = storage == 2 ? 16 : 8;
+    const int walkers = layers * nh * 2, least = storage == 2 ? 24 : 8;
     const bool runs = shift >= least && walkers < 1024;
     for (int d = d0; d < d1; d += runs ? shift : d1 - d0) {
         const int e = runs ? (d + shift < d1 ? d + shift : d1) : d1;
-#define DROP(ST_, HD_)                                                                                                  \
+#define DROP_T(ST_, HD_, TH_)                                                                                          \
     do {                                                                                                               \
-        constexpr int G_ = drop_blocks(ST_, HD_);                                                                      \
-        hipLaunchKernelGGL((k_kv_drop<ST_, HD_, G_>), dim3(nh * (runs ? (e - d + G_ - 1) / G_ : 1), layers, 2), dim3(256), 0, s, c, seq, nh, R, \
-                           st, d, e);                                                                                  \
+        constexpr int G_ = drop_blocks(ST_, HD_, TH_);                                                                 \
+        hipLaunchKernelGGL((k_kv_drop<ST_, HD_, G_, TH_>), dim3(nh * (runs ? (e - d + G_ - 1) / G_ : 1), layers, 2), dim3(TH_), 0, s, c, \
+                           seq, nh, R, st, d, e);                                                                      \
     } while (0)
+#define DROP(ST_, HD_) do { if (ST_ == 2 && !runs && walkers < 1024) DROP_T(ST_, HD_, ST_ == 2 ? 512 : 256); else DROP_T(ST_, HD_, 256); } while (0)
 #define DROP2(ST_) do { if (hd == 128) DROP(ST_, 128); else DROP(ST_, 64); } while (0)
         if (storage == 0) DROP2(0);
         else if (storage == 1) DROP2(1);
         else DROP2(2);
 #undef DROP2
 #undef DROP
+#undef DROP_T
     }
 }

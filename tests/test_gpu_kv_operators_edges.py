@@ -354,3 +354,23 @@ def test_attention_over_nan_and_infinite_rows(sd):
     sees = ref.ancestors(parent)[:, 3].cuda()
     assert torch.equal(torch.isnan(out[0, :, 0]).all(dim=1), sees) and torch.equal(out[0, ~sees], clean[0, ~sees])
     assert torch.equal(out[:, :, 1:], clean[:, :, 1:])
+
+
+@pytest.mark.parametrize("dtype,rows", FORMATS)
+@pytest.mark.parametrize("heads,dim", [(4, 64), (2, 128)])
+@pytest.mark.parametrize("ranges", [[(100, 800)], [(31, 770), (1000, 1), (1900, 200)], [(0, 1025), (1200, 900)]])
+def test_longer_gaps_are_closed_in_runs(sd, dtype, rows, heads, dim, ranges):
+    n = 3500
+    model = model_of(sd, layers=2, heads=heads, dim=dim, dtype=dtype)
+    kv = sd.KVCache(model, 2, 3600, rows=rows)
+    x = layers_of(2, n, heads, dim, 17, dtype)
+    kv.write_layers(1, 0, *(t.cuda() for t in x))
+    kv.set_len([0, n])
+    kv.drop_rows(1, ranges)
+    left = n - sum(c for _, c in ranges)
+    assert kv.len() == [0, left]
+    for p, got in enumerate(kv.read_layers(1, 0, left)):
+        for l in range(2):
+            want = after_drop(held(x[p], rows)[l], n, ranges, 1e4, p, dtype, rows)
+            off = (got[l].double().cpu() - want).abs()
+            assert bool((off <= (2.0 ** -23 * want.abs() + 1e-14 if dtype == "f32" and p == 0 else 0.0 * want)).all()), float(off.max())
