@@ -75,7 +75,7 @@ void launch_kv_fork(const KvPlanes& src, const KvPlanes& dst, const SeqList& to,
 // Bound: a run by loads, stores and some 350 vector instructions a wave and block together (the float64 turn is a third of them): 128
 // blocks of 4 layers, 32 heads of 128 dims, 268 MB in 85 - 92 us, 51 at the copy rate. A walk by its turns, each a chain of memory round
 // trips and the conversions of one workgroup, some 4 us: 130 of 700 rows of the same, 18 blocks, four at a time, 27 us. A walk's V blocks
-// of several shifts go by themselves, through LDS: that is 8 us for eight blocks.
+// of several shifts go by themselves, through LDS (a whole turn of four that way: 3 us more).
 // d rounded to odd: cut to 24 bits, the last one set if anything was cut, so that a later rounding to fewer bits sees on which side
 // of a border d lies. (From the bits: below 29 bits of a float64's fraction, a float32's ends.)
 static __device__ __forceinline__ float odd_float(double d) {
