@@ -10,7 +10,7 @@
 //     dims there is room for four, which are not faster (24.8 us, 24.6: eight ragged sequences of 32 rows).
 // Bound by the codes' stream where they are many: 134 MB in 32 us (one row over 16384, 32 heads of 128 dims; the same card streams a
 // plain read in 19), 176 MB in 43 (eight ragged sequences of 32 rows, whose parts are whole blocks of work: the longest part has 51, the
-// mean 40), 140 MB in 40 - 42 (64 rows over 16873). Some 7 us are fixed: launch, first loads, the waves' and the parts' merges.
+// mean 40), 140 MB in 39 - 42 (64 rows over 16873). Some 7 us are fixed: launch, first loads, the waves' and the parts' merges.
 // S^T = K Q^T puts query t in lane t % 32; exp(S) in its accumulator registers is the next product's operand (values are stored
 // with their rows in that order).
 #include "attn8.h"
@@ -34,7 +34,7 @@ struct Attn8Args {
 
 // grid (head, entry of the split x block of 32 query rows): the workgroups of a head share an XCD where heads are a multiple of eight, and
 // the query blocks of a part follow one another, so that all but the first find its rows in the caches. (Two query blocks a workgroup,
-// eight waves, and a launch that merges: 64 rows over 1280 / 16873 17.5 / 39.1 us, here 16.4 / 39.9 - 42; in a step's own launch, 64 rows
+// eight waves, and a launch that merges: 64 rows over 1280 / 16873 17.5 / 39.1 us, here 15.8 - 16.4 / 39.3 - 42; in a step's own launch, 64 rows
 // over some 600, 10.3 us, here 8.9.) Wave w has wave w of the part's blocks. NAT: natural rows; else packed ones.
 template <int HD, bool NAT>
 __global__ __launch_bounds__(256, 2) void k_attn8(Attn8Args a) {
